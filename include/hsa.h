@@ -53,7 +53,8 @@ typedef enum {
   HSA_ERR_UNSUPPORTED = -3,    /* valid request this build does not implement                   */
   HSA_ERR_CUDA = -4,           /* a CUDA runtime / driver call failed (see hsa_last_cuda_error)  */
   HSA_ERR_DEVICE_TIMEOUT = -5, /* a bounded device-side wait expired (status word)              */
-  HSA_ERR_DEVICE_BOUNDS = -6   /* a device-side index was out of range and was skipped          */
+  HSA_ERR_DEVICE_BOUNDS = -6,  /* a device-side index was out of range and was skipped          */
+  HSA_ERR_DEVICE_NONFINITE = -7 /* a value to be stored in 8 bits was not finite (or past 2^60)   */
 } hsa_status;
 
 /* lin_mode */
@@ -334,6 +335,176 @@ int hsa_safe_pass_tiles(hsa_ctx* ctx, int64_t* count_out);
 int hsa_last_cuda_error(hsa_ctx* ctx);
 
 int hsa_destroy(hsa_ctx* ctx);
+
+/* ------------------------------------------------------------------ rotary positions
+ * Row x of a head at position pos:  pair p of its first rot_dim values turns by
+ *     angle_p = pos[axis(p)] * f_p
+ *     (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ * and the other values stay.  The pairs are (i, i + rot_dim / 2) in the half layout, (2 i, 2 i + 1) in the
+ * interleaved one.  They are dealt out in order to n_axes position axes (one for a sequence; frame, row and
+ * column for video tokens), axis_pairs[a] of them to axis a, whose i-th pair has f = base^(-i / axis_pairs[a]).
+ * Frequencies are kept as turns per position in 64-bit fractions of a turn, and pos * turns is taken modulo one
+ * turn in whole numbers, so that far positions lose nothing: the angle is off by less than 2^-30 of a turn
+ * anywhere in the int32 range. */
+#define HSA_ROPE_HALF 0
+#define HSA_ROPE_INTERLEAVED 1
+
+/* scaling of the frequencies for contexts longer than the trained one, by `factor` s >= 1 */
+#define HSA_ROPE_SCALE_NONE 0
+#define HSA_ROPE_SCALE_LINEAR 1  /* f / s */
+#define HSA_ROPE_SCALE_BASE 2    /* base * s^(n / (n - 1)) for the n >= 2 pairs of an axis: the first keeps its
+                                    frequency, the last is divided by s */
+#define HSA_ROPE_SCALE_BANDS 3   /* with r = trained_tokens * f / 2 pi turns over the trained context:
+                                    g = clamp((r - beta_slow) / (beta_fast - beta_slow), 0, 1),
+                                    f (g + (1 - g) / s), amplitude 0.1 ln s + 1 */
+typedef struct {
+  int32_t head_dim;       /* a multiple of 8, 8..512                                            */
+  int32_t rot_dim;        /* even, 2..head_dim                                                  */
+  int32_t layout;         /* HSA_ROPE_HALF or HSA_ROPE_INTERLEAVED                              */
+  int32_t n_axes;         /* 1..3                                                               */
+  int32_t axis_pairs[3];  /* >= 0, sum rot_dim / 2 (n_axes of them are read)                    */
+  int32_t scaling;        /* HSA_ROPE_SCALE_*                                                   */
+  double base;            /* > 1                                                                */
+  double factor;          /* >= 1 (read unless NONE)                                            */
+  double trained_tokens;  /* BANDS: > 0                                                         */
+  double beta_fast;       /* BANDS: > beta_slow >= 0                                            */
+  double beta_slow;
+} hsa_rope_config;
+
+/* The table of a configuration, on the host: turns_host uint64[rot_dim / 2], amplitude_host one float. */
+int hsa_rope_table(const hsa_rope_config* cfg, uint64_t* turns_host, float* amplitude_host);
+
+/* What a call needs of it.  positions_dev: device int32 [n_axes][tokens], axis_stride elements apart; NULL:
+ * token i of a call stands at position i (of hsa_kv8_append: at its place in the sequence) on every axis. */
+typedef struct {
+  int32_t rot_dim, layout, n_axes;
+  int32_t axis_pairs[3];
+  float amplitude;
+  const uint64_t* turns_dev;     /* device uint64[rot_dim / 2], 8-byte aligned */
+  const int32_t* positions_dev;
+  int64_t axis_stride;           /* >= tokens where n_axes > 1 */
+} hsa_rope_args;
+
+#define HSA_TYPE_BF16 0
+#define HSA_TYPE_FP16 1
+#define HSA_TYPE_FP32 2
+
+/* hsa_rope flags: rotate by the negative angles (the transposed map).  The gradient of x is the transposed
+ * rotation of the gradient of the result, amplitude included. */
+#define HSA_ROPE_TRANSPOSE 1u
+
+/* out[token][head] = rotated x[token][head], computed in fp32 and rounded once.  x and out: device tensors of
+ * `type` (HSA_TYPE_*), [n_tokens][num_heads][head_dim] with element strides >= head_dim and unit dim stride;
+ * addresses and byte strides multiples of 16.  out == x with the same strides rotates in place; otherwise the
+ * two must not overlap.  n_tokens 0 does nothing. */
+int hsa_rope(const void* x, void* out, int32_t type, int32_t n_tokens, int32_t num_heads, int32_t head_dim,
+             int64_t tok_stride, int64_t head_stride, int64_t out_tok_stride, int64_t out_head_stride,
+             const hsa_rope_args* rope, uint32_t flags, void* stream);
+
+/* ------------------------------------------------------------------ history in 8 bits
+ * A paged cache of keys and values as e4m3 codes, for many sequences over one pool and for fewer key heads than
+ * query heads.  A page holds 64 tokens of every key head; the 64 x head_dim values of one (page, head) share a
+ * scale, a power of two: value = code * scale.  Block b of sequence s (tokens [64 b, 64 b + 64)) stands in page
+ * page_table[s][b].  The context keeps no lengths: the caller says in device memory how many tokens each sequence
+ * holds, so that a captured graph serves any lengths.
+ *
+ *     hsa_rope         (queries)
+ *     hsa_kv8_append   (keys, rotated on the way, and values -> pages; key sums)
+ *     hsa_kv8_attend   (softmax attention over all blocks, or over those a selection names)
+ *
+ * The key sums have the layout that hsa_select_blocks_noalloc reads, so one sequence's lists can come from there.
+ * Conventions as for hsa_ctx; calls of one context that are not ordered on the GPU must not overlap (they share
+ * the workspace, and an append writes the pools). */
+typedef struct hsa_kv8 hsa_kv8;
+
+typedef struct {
+  int32_t num_heads;      /* query heads: a multiple of num_kv_heads, at most 1024                       */
+  int32_t num_kv_heads;   /* key heads; query head h reads key head h / (num_heads / num_kv_heads)       */
+  int32_t head_dim;       /* 64 or 128                                                                   */
+  int32_t page_tokens;    /* must be HSA_PAGE_TOKENS                                                     */
+  int32_t max_pages;      /* pages of the pools                                                          */
+  int32_t max_blocks;     /* row length of the page table: blocks a sequence can hold                    */
+  int32_t max_batch;      /* sequences of a call, at most 4096                                           */
+  int32_t max_tokens;     /* new tokens or queries of a call, all sequences together                     */
+  float softmax_scale;    /* 0 -> 1/sqrt(head_dim)                                                       */
+  uint32_t flags;         /* must be 0                                                                   */
+} hsa_kv8_config;
+
+typedef struct {
+  size_t k_pool;      /* bytes: e4m3 [max_pages][num_kv_heads][64][head_dim]       */
+  size_t v_pool;      /* same                                                      */
+  size_t k_scale;     /* fp32 [max_pages][num_kv_heads]                            */
+  size_t v_scale;     /* same                                                      */
+  size_t page_table;  /* int32 [max_batch][max_blocks]                             */
+  size_t ksum;        /* fp32 [max_batch][num_kv_heads][max_blocks][head_dim]      */
+  size_t workspace;   /* status word, partial results of work split over CTAs      */
+} hsa_kv8_sizes;
+
+typedef struct {
+  void* k_pool;               /* device, 256-byte aligned                                     */
+  void* v_pool;
+  float* k_scale;             /* device, 16-byte aligned                                      */
+  float* v_scale;
+  const int32_t* page_table;  /* device, 16-byte aligned; the caller fills it                 */
+  float* ksum;                /* device, 16-byte aligned, or NULL: no key sums are kept       */
+  void* workspace;            /* device, 256-byte aligned                                     */
+} hsa_kv8_buffers;
+
+int hsa_kv8_query_sizes(const hsa_kv8_config* cfg, hsa_kv8_sizes* out);
+
+/* Creates a context over caller-owned device buffers of the current device.  Clears the status word and the
+ * counters of the workspace, synchronously; the pools may hold anything (a page is not read before it was
+ * written). */
+int hsa_kv8_create(hsa_kv8** out, const hsa_kv8_config* cfg, const hsa_kv8_buffers* bufs);
+
+/* Writes n_tokens new tokens of `batch` sequences.  Sequence s has the rows [token_start[s], token_start[s + 1])
+ * of k and v, which stand behind the held[s] tokens it holds.
+ *   k, v              device bf16 [n_tokens][num_kv_heads][head_dim], strides as hsa_append_kv
+ *   token_start_dev   device int32[batch + 1], ascending, or NULL: every sequence has n_tokens / batch rows
+ *   max_new           most rows of one sequence (the launch is sized by it); 1..n_tokens.  n_tokens 0 does nothing
+ *   held_dev          device int32[batch], read and not changed
+ *   rope              rotation of the keys (positions_dev: one column per row of k), or NULL for none
+ * A block that the call begins: its scale is the smallest power of two, at least 2^-48, by which no code passes
+ * 448, and the rows behind the call's last one are zeros.  A block that holds tokens already: its scale grows
+ * when the new rows need it, and the codes in it follow (exactly, but for values that become subnormal); it never
+ * shrinks.  Codes are rounded to nearest even from the fp32 rotated value.  With key sums: ksum[s][h][block] is
+ * the sum of the block's keys, this call's before rounding and earlier ones as they are stored.
+ * Appending the same rows again over the same held[] leaves the same bits.  The pages of different sequences that
+ * a call writes must be distinct; full pages may be shared.
+ * Values that are not finite or pass 2^60 are stored as 0 (NaN) or at 2^60 and HSA_ERR_DEVICE_NONFINITE is left in the
+ * status word.  A sequence whose rows or lengths do not fit (token_start not ascending or past n_tokens, more than
+ * max_new rows, held < 0, more than max_blocks blocks) is left out as a whole, a page id outside the pools as that
+ * page, with HSA_ERR_DEVICE_BOUNDS. */
+int hsa_kv8_append(hsa_kv8* ctx, const void* k, const void* v, int32_t n_tokens, int32_t batch, int64_t tok_stride,
+                   int64_t head_stride, const int32_t* token_start_dev, int32_t max_new, const int32_t* held_dev,
+                   const hsa_rope_args* rope, void* stream);
+
+/* out[i][h] = sum_j softmax_j(scale q[i][h] . k_j) v_j over the tokens j of query i's sequence that it sees.
+ *   q, out           device bf16 [n_tokens][num_heads][head_dim], own strides each
+ *   token_start_dev  as above: the queries of each sequence; max_q most of one sequence
+ *   lengths_dev      device int32[batch]: tokens each sequence holds, its queries' own tokens included
+ *   causal           query i of n of a sequence of length L stands at L - n + i and sees the tokens up to itself;
+ *                    0: all L
+ *   sel_idx_dev      device int32[batch][num_kv_heads][max_topk] block lists, or NULL: every block
+ *   sel_cnt_dev      device int32[batch][num_kv_heads] their lengths (clamped to 0..max_topk)
+ *   lse_dev          device fp32 [n_tokens][num_heads] receiving ln sum_j exp(scale q . k_j), or NULL
+ * A block that a list names twice counts twice.  A query that sees nothing gets zeros and an lse of -inf.  Rows of
+ * out that belong to no sequence are left as they were.  What the result is made of: products exact, sums in fp32,
+ * softmax weights rounded to 8 significant bits or more (see the kernels).  Sequences that do not fit (as above,
+ * lengths < 0 or past max_blocks) are left out, list entries outside [0, max_blocks) and pages outside the pools count
+ * as not seen, both with HSA_ERR_DEVICE_BOUNDS; list entries behind the length see nothing. */
+int hsa_kv8_attend(hsa_kv8* ctx, const void* q, int32_t n_tokens, int32_t batch, int64_t tok_stride,
+                   int64_t head_stride, const int32_t* token_start_dev, int32_t max_q, const int32_t* lengths_dev,
+                   int32_t causal, const int32_t* sel_idx_dev, const int32_t* sel_cnt_dev, int32_t max_topk, void* out,
+                   int64_t out_tok_stride, int64_t out_head_stride, float* lse_dev, void* stream);
+
+/* Synchronises the device, reads and clears the status word: HSA_OK or a DEVICE_* code. */
+int hsa_kv8_device_status(hsa_kv8* ctx, int32_t* status_out);
+
+/* Last CUDA error code recorded by a failing call on this context (0 if none). */
+int hsa_kv8_last_cuda_error(hsa_kv8* ctx);
+
+int hsa_kv8_destroy(hsa_kv8* ctx);
 
 const char* hsa_status_string(int status);
 

@@ -920,6 +920,7 @@ const char* hsa_status_string(int s) {
     case HSA_ERR_CUDA: return "CUDA error";
     case HSA_ERR_DEVICE_TIMEOUT: return "device-side wait timed out";
     case HSA_ERR_DEVICE_BOUNDS: return "device-side index out of range";
+    case HSA_ERR_DEVICE_NONFINITE: return "value to be stored in 8 bits not finite or past 2^60";
     default: return "unknown status";
   }
 }

@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -28,12 +28,17 @@ HSA_ERR_UNSUPPORTED = -3
 HSA_ERR_CUDA = -4
 HSA_ERR_DEVICE_TIMEOUT = -5
 HSA_ERR_DEVICE_BOUNDS = -6
+HSA_ERR_DEVICE_NONFINITE = -7
 HSA_LIN_NONE, HSA_LIN_STATE, HSA_LIN_LINFORMER = 0, 1, 2
 HSA_PHI_ELU1, HSA_PHI_RELU = 0, 1
 HSA_CFG_CAUSAL = 1
 HSA_CFG_ADAPTIVE = 2
 HSA_CFG_GRID_BARRIER_SELECT = 4
 HSA_FWD_NO_LINEAR, HSA_FWD_NO_SPARSE = 1, 2
+HSA_ROPE_HALF, HSA_ROPE_INTERLEAVED = 0, 1
+HSA_ROPE_SCALE_NONE, HSA_ROPE_SCALE_LINEAR, HSA_ROPE_SCALE_BASE, HSA_ROPE_SCALE_BANDS = 0, 1, 2, 3
+HSA_ROPE_TRANSPOSE = 1
+HSA_TYPE_BF16, HSA_TYPE_FP16, HSA_TYPE_FP32 = 0, 1, 2
 PAGE_TOKENS = 64
 TILE_M = 128
 
@@ -47,6 +52,9 @@ EXPORTS = [
     "hsa_device_status", "hsa_safe_pass_tiles",
     "hsa_last_cuda_error",
     "hsa_destroy", "hsa_status_string",
+    "hsa_rope_table", "hsa_rope",
+    "hsa_kv8_query_sizes", "hsa_kv8_create", "hsa_kv8_append", "hsa_kv8_attend", "hsa_kv8_device_status",
+    "hsa_kv8_last_cuda_error", "hsa_kv8_destroy",
 ]
 
 
@@ -73,6 +81,34 @@ class hsa_buffers(C.Structure):
     _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("state", C.c_void_p),
                 ("workspace", C.c_void_p), ("kc_pool", C.c_void_p), ("vc_pool", C.c_void_p),
                 ("e_k", C.c_void_p), ("e_v", C.c_void_p)]
+
+
+class hsa_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("n_axes", C.c_int32),
+                ("axis_pairs", C.c_int32 * 3), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("trained_tokens", C.c_double), ("beta_fast", C.c_double), ("beta_slow", C.c_double)]
+
+
+class hsa_rope_args(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("layout", C.c_int32), ("n_axes", C.c_int32), ("axis_pairs", C.c_int32 * 3),
+                ("amplitude", C.c_float), ("turns_dev", C.c_void_p), ("positions_dev", C.c_void_p),
+                ("axis_stride", C.c_int64)]
+
+
+class hsa_kv8_config(C.Structure):
+    _fields_ = [("num_heads", C.c_int32), ("num_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_tokens", C.c_int32),
+                ("max_pages", C.c_int32), ("max_blocks", C.c_int32), ("max_batch", C.c_int32), ("max_tokens", C.c_int32),
+                ("softmax_scale", C.c_float), ("flags", C.c_uint32)]
+
+
+class hsa_kv8_sizes(C.Structure):
+    _fields_ = [("k_pool", C.c_size_t), ("v_pool", C.c_size_t), ("k_scale", C.c_size_t), ("v_scale", C.c_size_t),
+                ("page_table", C.c_size_t), ("ksum", C.c_size_t), ("workspace", C.c_size_t)]
+
+
+class hsa_kv8_buffers(C.Structure):
+    _fields_ = [("k_pool", C.c_void_p), ("v_pool", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("page_table", C.c_void_p), ("ksum", C.c_void_p), ("workspace", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -110,6 +146,15 @@ def _load() -> C.CDLL:
     lib.hsa_destroy.argtypes = [vp]
     lib.hsa_status_string.argtypes = [C.c_int]
     lib.hsa_status_string.restype = C.c_char_p
+    lib.hsa_rope_table.argtypes = [C.POINTER(hsa_rope_config), vp, C.POINTER(C.c_float)]
+    lib.hsa_rope.argtypes = [vp, vp, i32, i32, i32, i32, i64, i64, i64, i64, C.POINTER(hsa_rope_args), u32, vp]
+    lib.hsa_kv8_query_sizes.argtypes = [C.POINTER(hsa_kv8_config), C.POINTER(hsa_kv8_sizes)]
+    lib.hsa_kv8_create.argtypes = [C.POINTER(vp), C.POINTER(hsa_kv8_config), C.POINTER(hsa_kv8_buffers)]
+    lib.hsa_kv8_append.argtypes = [vp, vp, vp, i32, i32, i64, i64, vp, i32, vp, C.POINTER(hsa_rope_args), vp]
+    lib.hsa_kv8_attend.argtypes = [vp, vp, i32, i32, i64, i64, vp, i32, vp, i32, vp, vp, i32, vp, i64, i64, vp, vp]
+    lib.hsa_kv8_device_status.argtypes = [vp, C.POINTER(i32)]
+    lib.hsa_kv8_last_cuda_error.argtypes = [vp]
+    lib.hsa_kv8_destroy.argtypes = [vp]
     for name in EXPORTS:
         if name != "hsa_status_string":
             getattr(lib, name).restype = C.c_int
@@ -141,6 +186,12 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 def _stream() -> int:
     # the current stream of the current device, without building a torch.cuda.Stream (3.1 -> 0.2 us a call)
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def _on_current(t: torch.Tensor, name: str) -> None:
+    """The calls enqueue on the current stream of the current device: refuses a tensor of another one."""
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name}: on {t.device}, which is not the current device (use torch.cuda.device)")
 
 
 def _thd(t: torch.Tensor, name: str) -> Tuple[int, int]:
@@ -313,6 +364,77 @@ def hsa_destroy(ctx: int) -> None:
     _check(_lib.hsa_destroy(ctx), "hsa_destroy")
 
 
+_TYPES = {torch.bfloat16: HSA_TYPE_BF16, torch.float16: HSA_TYPE_FP16, torch.float32: HSA_TYPE_FP32}
+
+
+def hsa_rope_table(cfg: hsa_rope_config) -> Tuple[torch.Tensor, float]:
+    """(turns per position of every pair, as the bits of uint64 in an int64 CPU tensor; amplitude)."""
+    turns = torch.zeros(max(1, min(cfg.rot_dim, 512) // 2), dtype=torch.int64)
+    amplitude = C.c_float()
+    _check(_lib.hsa_rope_table(C.byref(cfg), turns.data_ptr(), C.byref(amplitude)), "hsa_rope_table")
+    return turns, amplitude.value
+
+
+def hsa_rope(x: torch.Tensor, out: torch.Tensor, rope: hsa_rope_args, flags: int = 0) -> None:
+    """x, out: bf16, fp16 or fp32 [tokens, H, d] with unit dim stride; out may be x."""
+    if x.dtype not in _TYPES or out.dtype != x.dtype:
+        raise ValueError("hsa_rope: expected x and out of one type, bf16, fp16 or fp32")
+    if x.dim() != 3 or out.shape != x.shape or not x.is_cuda or out.device != x.device:
+        raise ValueError("hsa_rope: expected CUDA tensors [tokens, H, d] of one shape")
+    if x.stride(2) != 1 or out.stride(2) != 1:
+        raise ValueError("hsa_rope: expected unit dim stride")
+    _on_current(x, "x")
+    _check(_lib.hsa_rope(x.data_ptr(), out.data_ptr(), _TYPES[x.dtype], x.shape[0], x.shape[1], x.shape[2], x.stride(0),
+                         x.stride(1), out.stride(0), out.stride(1), C.byref(rope), int(flags), _stream()), "hsa_rope")
+
+
+def hsa_kv8_query_sizes(cfg: hsa_kv8_config) -> hsa_kv8_sizes:
+    out = hsa_kv8_sizes()
+    _check(_lib.hsa_kv8_query_sizes(C.byref(cfg), C.byref(out)), "hsa_kv8_query_sizes")
+    return out
+
+
+def hsa_kv8_create(cfg: hsa_kv8_config, bufs: hsa_kv8_buffers) -> int:
+    handle = C.c_void_p()
+    _check(_lib.hsa_kv8_create(C.byref(handle), C.byref(cfg), C.byref(bufs)), "hsa_kv8_create")
+    return handle.value
+
+
+def hsa_kv8_append(ctx: int, k: torch.Tensor, v: torch.Tensor, batch: int, token_start: Optional[torch.Tensor],
+                   max_new: int, held: torch.Tensor, rope: Optional[hsa_rope_args] = None) -> None:
+    ts, hs = _thd(k, "k")
+    if _thd(v, "v") != (ts, hs) or v.shape != k.shape:
+        raise ValueError("k and v must share shape and strides")
+    _check(_lib.hsa_kv8_append(ctx, k.data_ptr(), v.data_ptr(), k.shape[0], int(batch), ts, hs, _ptr(token_start),
+                               int(max_new), held.data_ptr(), C.byref(rope) if rope is not None else None, _stream()),
+           "hsa_kv8_append")
+
+
+def hsa_kv8_attend(ctx: int, q: torch.Tensor, batch: int, token_start: Optional[torch.Tensor], max_q: int,
+                   lengths: torch.Tensor, causal: bool, sel_idx: Optional[torch.Tensor], sel_cnt: Optional[torch.Tensor],
+                   out: torch.Tensor, lse: Optional[torch.Tensor] = None) -> None:
+    ts, hs = _thd(q, "q")
+    ots, ohs = _thd(out, "out")
+    _check(_lib.hsa_kv8_attend(ctx, q.data_ptr(), q.shape[0], int(batch), ts, hs, _ptr(token_start), int(max_q),
+                               lengths.data_ptr(), int(causal), _ptr(sel_idx), _ptr(sel_cnt),
+                               0 if sel_idx is None else sel_idx.shape[-1], out.data_ptr(), ots, ohs, _ptr(lse),
+                               _stream()), "hsa_kv8_attend")
+
+
+def hsa_kv8_device_status(ctx: int) -> int:
+    s = C.c_int32()
+    _check(_lib.hsa_kv8_device_status(ctx, C.byref(s)), "hsa_kv8_device_status")
+    return s.value
+
+
+def hsa_kv8_last_cuda_error(ctx: int) -> int:
+    return _lib.hsa_kv8_last_cuda_error(ctx)
+
+
+def hsa_kv8_destroy(ctx: int) -> None:
+    _check(_lib.hsa_kv8_destroy(ctx), "hsa_kv8_destroy")
+
+
 # ------------------------------------------------------------------ convenience wrapper
 class HSAContext:
     """One attention layer of one sequence: allocates the caller-owned buffers with torch and
@@ -480,6 +602,177 @@ class HSAContext:
     def destroy(self) -> None:
         if getattr(self, "ctx", None):
             hsa_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+_LAYOUTS = {"half": HSA_ROPE_HALF, "interleaved": HSA_ROPE_INTERLEAVED}
+_SCALINGS = {"none": HSA_ROPE_SCALE_NONE, "linear": HSA_ROPE_SCALE_LINEAR, "base": HSA_ROPE_SCALE_BASE,
+             "bands": HSA_ROPE_SCALE_BANDS}
+
+
+class RotaryPositions:
+    """Rotary positions of one layer: the frequency table on the device, and the calls that take it.
+
+    rot_dim      leading values of a head that turn (default: all of them)
+    layout       "half": pairs (i, i + rot_dim / 2); "interleaved": pairs (2 i, 2 i + 1)
+    axis_pairs   pairs of each position axis, 1 to 3 of them (default: one axis)
+    scaling      "none", "linear", "base" or "bands" with `factor` (see hsa_rope_config)
+    """
+
+    def __init__(self, head_dim: int, rot_dim: Optional[int] = None, layout: str = "half", base: float = 10000.0,
+                 axis_pairs: Optional[Sequence[int]] = None, scaling: str = "none", factor: float = 1.0,
+                 trained_tokens: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                 device: str | torch.device = "cuda:0"):
+        if layout not in _LAYOUTS or scaling not in _SCALINGS:
+            raise ValueError(f"layout {layout!r} or scaling {scaling!r} unknown")
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        pairs = [rot_dim // 2] if axis_pairs is None else [int(p) for p in axis_pairs]
+        if not 1 <= len(pairs) <= 3:
+            raise ValueError("axis_pairs: expected one to three axes")
+        self.n_axes = len(pairs)
+        axes = (C.c_int32 * 3)(*pairs, *[0] * (3 - len(pairs)))
+        self.cfg = hsa_rope_config(head_dim, rot_dim, _LAYOUTS[layout], self.n_axes, axes, _SCALINGS[scaling], base, factor,
+                                   trained_tokens, beta_fast, beta_slow)
+        turns, amplitude = hsa_rope_table(self.cfg)
+        self.turns = turns.to(device)
+        self.head_dim, self.device = head_dim, self.turns.device
+        self._args = (rot_dim, _LAYOUTS[layout], self.n_axes, axes, amplitude, self.turns.data_ptr())
+
+    def args(self, positions: Optional[torch.Tensor], n_tokens: int) -> hsa_rope_args:
+        """positions: int32 [tokens] or [axes, tokens] with unit token stride, or None: token i at position i."""
+        stride = 0
+        if positions is not None:
+            if positions.dtype != torch.int32 or positions.device != self.device:
+                raise ValueError("positions: expected int32 on the table's device")
+            if positions.dim() == 1 and self.n_axes == 1:
+                positions = positions[None]
+            if positions.dim() != 2 or positions.shape != (self.n_axes, n_tokens) or (n_tokens > 1 and positions.stride(1) != 1):
+                raise ValueError(f"positions: expected [{self.n_axes}, {n_tokens}] with unit token stride")
+            stride = positions.stride(0)
+        return hsa_rope_args(*self._args, _ptr(positions), stride)
+
+    def apply(self, x: torch.Tensor, positions: Optional[torch.Tensor] = None, transpose: bool = False,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rotates x [tokens, H, d]; transpose=True applies the transposed map, the gradient of the rotation."""
+        if x.dim() != 3 or x.shape[2] != self.head_dim or x.device != self.device:
+            raise ValueError(f"x: expected [tokens, H, {self.head_dim}] on {self.device}")
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        hsa_rope(x, out, self.args(positions, x.shape[0]), HSA_ROPE_TRANSPOSE if transpose else 0)
+        return out
+
+
+class KV8Cache:
+    """A paged cache of keys and values in 8 bits for one layer and many sequences; allocates what it is not given.
+
+    Buffers (attributes): k_codes, v_codes float8_e4m3fn [pages, kv heads, 64, d]; k_scale, v_scale fp32 [pages, kv heads];
+    page_table int32 [batch, blocks], which the caller fills; ksum fp32 [batch, kv heads, blocks, d] where key_sums is
+    True (or the tensor itself)."""
+
+    def __init__(self, num_heads: int, num_kv_heads: int, head_dim: int, max_pages: int, max_blocks: int, max_batch: int = 1,
+                 max_tokens: int = 1, softmax_scale: float = 0.0, device: str | torch.device = "cuda:0",
+                 page_table: Optional[torch.Tensor] = None, k_codes: Optional[torch.Tensor] = None,
+                 v_codes: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None, key_sums: bool | torch.Tensor | None = False):
+        self.ctx = None
+        dev = torch.device(device)
+        self.device = torch.device("cuda", torch.cuda.current_device()) if dev.index is None and dev.type == "cuda" else dev
+        self.num_heads, self.num_kv_heads, self.head_dim = num_heads, num_kv_heads, head_dim
+        self.max_pages, self.max_blocks, self.max_batch, self.max_tokens = max_pages, max_blocks, max_batch, max_tokens
+        self.cfg = hsa_kv8_config(num_heads, num_kv_heads, head_dim, PAGE_TOKENS, max_pages, max_blocks, max_batch,
+                                  max_tokens, softmax_scale, 0)
+        self.sizes = hsa_kv8_query_sizes(self.cfg)
+
+        def buffer(t, shape, dtype, name):
+            if t is None:
+                return torch.zeros(shape, dtype=dtype, device=self.device)
+            if tuple(t.shape) != shape or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+                raise ValueError(f"{name}: expected a contiguous {dtype} {list(shape)} on {self.device}")
+            return t
+
+        pool, per_page = (max_pages, num_kv_heads, PAGE_TOKENS, head_dim), (max_pages, num_kv_heads)
+        with torch.cuda.device(self.device):
+            self.k_codes = buffer(k_codes, pool, torch.float8_e4m3fn, "k_codes")
+            self.v_codes = buffer(v_codes, pool, torch.float8_e4m3fn, "v_codes")
+            self.k_scale = buffer(k_scale, per_page, torch.float32, "k_scale")
+            self.v_scale = buffer(v_scale, per_page, torch.float32, "v_scale")
+            self.page_table = buffer(page_table, (max_batch, max_blocks), torch.int32, "page_table")
+            self.ksum = None
+            if key_sums is not None and key_sums is not False:
+                self.ksum = buffer(None if key_sums is True else key_sums, (max_batch, num_kv_heads, max_blocks, head_dim),
+                                   torch.float32, "key_sums")
+            self.workspace = torch.empty(self.sizes.workspace, dtype=torch.uint8, device=self.device)
+            bufs = hsa_kv8_buffers(self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scale.data_ptr(),
+                                   self.v_scale.data_ptr(), self.page_table.data_ptr(), _ptr(self.ksum),
+                                   self.workspace.data_ptr())
+            self.ctx = hsa_kv8_create(self.cfg, bufs)
+
+    def _rows(self, t: torch.Tensor, heads: int, counts: torch.Tensor, token_start: Optional[torch.Tensor],
+              most: Optional[int], name: str) -> int:
+        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.device != self.device:
+            raise ValueError(f"{name}: expected [tokens, {heads}, {self.head_dim}] on {self.device}")
+        for x in (counts, token_start):
+            if x is not None and (x.dtype != torch.int32 or x.device != self.device or not x.is_contiguous() or x.dim() != 1):
+                raise ValueError("held, lengths, token_start: expected contiguous int32 vectors on the cache's device")
+        if token_start is not None and token_start.numel() != counts.numel() + 1:
+            raise ValueError("token_start: expected one entry more than there are sequences")
+        _on_current(t, name)
+        if most is not None:
+            return int(most)
+        return t.shape[0] if token_start is not None else t.shape[0] // max(1, counts.numel())
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, held: torch.Tensor, token_start: Optional[torch.Tensor] = None,
+               max_new: Optional[int] = None, rope: Optional[RotaryPositions] = None,
+               positions: Optional[torch.Tensor] = None) -> None:
+        """Appends k, v [tokens, kv heads, d] behind the held[s] tokens of each sequence (int32 [batch]); token_start
+        int32 [batch + 1] where the sequences' rows differ in number, at most max_new to one.  Keys are rotated by
+        `rope` at `positions` (default: their place in the sequence)."""
+        most = self._rows(k, self.num_kv_heads, held, token_start, max_new, "k")
+        if v.device != self.device or v.shape != k.shape:
+            raise ValueError("k and v must share shape and device")
+        if rope is not None and (rope.device != self.device or rope.head_dim != self.head_dim):
+            raise ValueError("rope: of another device or head size")
+        if rope is None and positions is not None:
+            raise ValueError("positions without rope")
+        hsa_kv8_append(self.ctx, k, v, held.numel(), token_start, most, held,
+                       None if rope is None else rope.args(positions, k.shape[0]))
+
+    def attend(self, q: torch.Tensor, lengths: torch.Tensor, token_start: Optional[torch.Tensor] = None,
+               max_q: Optional[int] = None, causal: bool = True, sel_idx: Optional[torch.Tensor] = None,
+               sel_cnt: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, with_lse: bool = False):
+        """Attention of q [tokens, heads, d] over the lengths[s] tokens of each sequence (the queries' own included);
+        sel_idx int32 [batch, kv heads, n] with sel_cnt int32 [batch, kv heads]: block lists.  Returns out, or
+        (out, lse fp32 [tokens, heads]) with with_lse.  A row that belongs to no sequence is not written."""
+        most = self._rows(q, self.num_heads, lengths, token_start, max_q, "q")
+        if (sel_idx is None) != (sel_cnt is None):
+            raise ValueError("sel_idx and sel_cnt belong together")
+        if sel_idx is not None:
+            lists = (lengths.numel(), self.num_kv_heads)
+            if tuple(sel_idx.shape[:-1]) != lists or tuple(sel_cnt.shape) != lists:
+                raise ValueError(f"sel_idx, sel_cnt: expected [{lists[0]}, {lists[1]}, n] and [{lists[0]}, {lists[1]}]")
+            for x in (sel_idx, sel_cnt):
+                if x.dtype != torch.int32 or x.device != self.device or not x.is_contiguous():
+                    raise ValueError("sel_idx, sel_cnt: expected contiguous int32 on the cache's device")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.device != q.device:
+            raise ValueError("out: expected the shape and device of q")
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
+        hsa_kv8_attend(self.ctx, q, lengths.numel(), token_start, most, lengths, causal, sel_idx, sel_cnt, out, lse)
+        return (out, lse) if with_lse else out
+
+    def device_status(self) -> int:
+        return hsa_kv8_device_status(self.ctx)
+
+    def destroy(self) -> None:
+        if getattr(self, "ctx", None):
+            hsa_kv8_destroy(self.ctx)
             self.ctx = None
 
     def __del__(self):
