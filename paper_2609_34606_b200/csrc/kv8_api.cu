@@ -14,6 +14,7 @@ struct hsa_kv8 {
   hsa_kv8_buffers buf;
   float scale;
   int dev, nsm;
+  CUtensorMap tm_k, tm_v;
   int last_cuda_error;
 };
 
@@ -58,7 +59,28 @@ bool on_device(hsa_kv8* ctx) {
   return cudaGetDevice(&dev) == cudaSuccess && dev == ctx->dev;
 }
 
-constexpr size_t kStatusBytes = 256;
+// workspace: status word, tickets, parts
+constexpr int kMaxCtas = 160;  // CTAs of an attention launch (one to an SM)
+constexpr size_t kStatusBytes = 256, kTicketBytes = 1024;
+static_assert(kMaxCtas * 4 <= kTicketBytes, "a ticket to a CTA");
+
+size_t part_floats(const hsa_kv8_config* c) { return kv8_decode_slot(c->head_dim); }
+
+// A pool as rows of head_dim bytes, read a page tile (64 rows) at a time into the swizzle that spans a row.
+bool encode_pool(CUtensorMap* tm, void* base, uint64_t rows, int D) {
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult q;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+    return false;
+  const auto enc = reinterpret_cast<CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill)>(p);
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(D), rows}, strides[1] = {static_cast<cuuint64_t>(D)};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(D), kBlock}, ones[2] = {1, 1};
+  return enc(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 }  // namespace
 
@@ -71,7 +93,7 @@ int hsa_kv8_query_sizes(const hsa_kv8_config* cfg, hsa_kv8_sizes* out) {
   out->k_scale = out->v_scale = pages * H * 4;
   out->page_table = static_cast<size_t>(cfg->max_batch) * cfg->max_blocks * 4;
   out->ksum = static_cast<size_t>(cfg->max_batch) * H * cfg->max_blocks * D * 4;
-  out->workspace = kStatusBytes;
+  out->workspace = kStatusBytes + kTicketBytes + 2 * kMaxCtas * part_floats(cfg) * 4;
   return HSA_OK;
 }
 
@@ -96,10 +118,13 @@ int hsa_kv8_create(hsa_kv8** out, const hsa_kv8_config* cfg, const hsa_kv8_buffe
   ctx->dev = dev;
   ctx->nsm = nsm;
   ctx->last_cuda_error = 0;
-  cudaError_t e = cudaMemset(b->workspace, 0, kStatusBytes);
+  cudaError_t e = cudaMemset(b->workspace, 0, kStatusBytes + kTicketBytes);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = kv8_append_init(cfg->head_dim);
-  if (e != cudaSuccess) {
+  if (e == cudaSuccess) e = kv8_decode_init(cfg->head_dim);
+  const uint64_t rows = static_cast<uint64_t>(cfg->max_pages) * cfg->num_kv_heads * kBlock;
+  if (e != cudaSuccess || !encode_pool(&ctx->tm_k, b->k_pool, rows, cfg->head_dim) ||
+      !encode_pool(&ctx->tm_v, b->v_pool, rows, cfg->head_dim)) {
     delete ctx;
     return HSA_ERR_CUDA;
   }
@@ -177,7 +202,15 @@ int hsa_kv8_attend(hsa_kv8* ctx, const void* q, int32_t n_tokens, int32_t batch,
   a.k_scale = ctx->buf.k_scale;
   a.v_scale = ctx->buf.v_scale;
   a.status = static_cast<int32_t*>(ctx->buf.workspace);
-  const cudaError_t e = launch_kv8_attend_plain(a, c.head_dim, static_cast<cudaStream_t>(stream));
+  uint8_t* ws = static_cast<uint8_t*>(ctx->buf.workspace);
+  Kv8Work w{};
+  w.tickets = reinterpret_cast<int32_t*>(ws + kStatusBytes);
+  w.parts = reinterpret_cast<float*>(ws + kStatusBytes + kTicketBytes);
+  const int ctas = ctx->nsm < kMaxCtas ? ctx->nsm : kMaxCtas;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = static_cast<int64_t>(max_q) * a.group <= kv8_decode_rows(c.head_dim)
+                            ? launch_kv8_decode(a, w, c.head_dim, ctas, ctx->tm_k, ctx->tm_v, st)
+                            : launch_kv8_attend_plain(a, c.head_dim, st);
   return e == cudaSuccess ? HSA_OK : cuda_fail(ctx, e);
 }
 
@@ -186,7 +219,7 @@ int hsa_kv8_device_status(hsa_kv8* ctx, int32_t* status_out) {
   int32_t v = 0;
   cudaError_t e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = cudaMemcpy(&v, ctx->buf.workspace, 4, cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess && v != 0) e = cudaMemset(ctx->buf.workspace, 0, kStatusBytes);
+  if (e == cudaSuccess && v != 0) e = cudaMemset(ctx->buf.workspace, 0, kStatusBytes + kTicketBytes);
   if (e != cudaSuccess) return cuda_fail(ctx, e);
   *status_out = v;
   return HSA_OK;
