@@ -97,15 +97,15 @@ def append(state, table, held, rows_k, rows_v):
 
 # ------------------------------------------------------------------ attention
 def attend(q, state, table, lengths, causal, scale=None, sel=None):
-    """q: list of [n, Hq, d] per sequence; sel[s][kv head]: block ids, or None.  Returns per sequence (out, lse,
-    spread): spread [n, Hq, d] is the weighted mean of |v|, by which rounding errors are measured."""
+    """q: list of [n, Hq, d] per sequence; sel[s][kv head]: block ids, or None.  Returns per sequence (out, lse, spread,
+    size), the last two by which rounding errors are measured: the weighted mean of |v| and the sum of |v| over the keys."""
     Hkv, d = state["k_scale"].shape[1], state["k_codes"].shape[-1]
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     res = []
     for s, length in enumerate(lengths):
         x = np.asarray(q[s], dtype=np.float64)
         n, Hq = x.shape[0], x.shape[1]
-        out, spread = np.zeros((n, Hq, d)), np.zeros((n, Hq, d))
+        out, spread, size = np.zeros((n, Hq, d)), np.zeros((n, Hq, d)), np.zeros((n, Hq, d))
         lse = np.full((n, Hq), -np.inf)
         for h in range(Hkv):
             blocks = list(range((length + BLOCK - 1) // BLOCK)) if sel is None else [int(b) for b in sel[s][h]]
@@ -127,6 +127,7 @@ def attend(q, state, table, lengths, causal, scale=None, sel=None):
                     total = w.sum()
                     out[i, r] = w @ v[see] / total
                     spread[i, r] = w @ np.abs(v[see]) / total
+                    size[i, r] = np.abs(v[see]).sum(0)
                     lse[i, r] = top + math.log(total)
-        res.append((out, lse, spread))
+        res.append((out, lse, spread, size))
     return res
