@@ -79,14 +79,16 @@ struct Kv8AttendArgs {
 // token r / group of the sequence and query head h * group + r % group, so that query heads of one key head read its pages
 // once.  An item has as many steps as it has pages to read (times kv8 pages a step).  The steps of all items, in order,
 // are cut into equal runs, one for each CTA, from the lengths as they stand in device memory: whatever the batch holds,
-// every SM gets the same share and a captured graph serves any lengths.  An item that lies in one CTA's run is written by
+// every SM gets the same share and a captured graph serves any lengths.  (Where there are CTAs for it, each item is cut by
+// itself into parts of min_steps at least: a run that crosses items would make some wait for others.)  An item that lies in one CTA's run is written by
 // it; of one that is cut, each CTA leaves an unnormalised part in the workspace and the last to take a ticket joins them in
 // the order of the runs, which makes the result independent of which CTA that is.  Nobody waits.
 struct Kv8Work {
   int tile_rows;       // query rows of an item
   int tiles;           // tiles of a sequence with max_rows rows
   int step_pages;
-  int min_steps;       // no run is shorter
+  int min_steps;       // an item is not cut into shorter parts while there is a CTA for each part
+  int item_steps;      // steps that an item costs beside its own: runs are cut as if they came before them
   int64_t items;       // batch * Hkv * tiles
   float* parts;        // [2 * CTAs][slot_floats]
   int64_t slot_floats;
@@ -117,8 +119,9 @@ struct Kv8Item {
 
 __device__ __forceinline__ Kv8Item kv8_item(const Kv8AttendArgs& a, const Kv8Work& w, int64_t i) {
   Kv8Item it;
-  it.tile = static_cast<int>(i % w.tiles);
-  const int bh = static_cast<int>(i / w.tiles);
+  const uint32_t at = static_cast<uint32_t>(i);  // (launches with 2^31 items are refused)
+  it.tile = static_cast<int>(at % static_cast<uint32_t>(w.tiles));
+  const int bh = static_cast<int>(at / static_cast<uint32_t>(w.tiles));
   it.b = bh / a.Hkv;
   it.h = bh % a.Hkv;
   it.steps = it.pages = 0;
@@ -143,40 +146,112 @@ __device__ __forceinline__ Kv8Item kv8_item(const Kv8AttendArgs& a, const Kv8Wor
   return it;
 }
 
-struct Kv8Run {
-  int64_t lo, hi;      // the CTA's steps
-  int64_t share;
-  int64_t item, start; // the item that `lo` lies in, and where its steps begin
+// A stretch of an item that one CTA does.
+struct Kv8Segment {
+  Kv8Item it;
+  int s0, s1;                   // steps of the item
+  int first_cta, last_cta;      // CTAs that the item is shared by
+  __device__ __forceinline__ bool whole() const { return first_cta == last_cta; }
+  // where this CTA's part of the item goes: each has at most one item that began earlier and one that goes on
+  __device__ __forceinline__ int64_t slot() const { return 2 * static_cast<int64_t>(blockIdx.x) + (s0 == 0 ? 1 : 0); }
+  __device__ __forceinline__ static int64_t slot_of(int cta, int first) { return 2 * static_cast<int64_t>(cta) + (cta == first ? 1 : 0); }
 };
 
-// The CTA's run; all THREADS threads call it.  lo >= hi: nothing to do.
+constexpr int kSegments = 32;   // of a CTA, worked out in advance; what goes beyond is worked out by each role as it gets there
+
+// The CTA's run, in shared memory.
+struct Kv8Plan {
+  int64_t hi, share;            // behind the CTA's last step; steps of a CTA (those that items cost beside their own included)
+  int n;                        // segments below
+  bool more;                    // further ones follow, from item more_item on, whose steps begin at more_start
+  int64_t more_item, more_start;
+  Kv8Segment seg[kSegments];
+};
+
+__device__ __forceinline__ void kv8_cut(Kv8Segment* g, int64_t start, int64_t lo, int64_t hi, int64_t share) {
+  const int64_t end = start + g->it.steps;
+  g->s0 = static_cast<int>(max(lo - start, static_cast<int64_t>(0)));
+  g->s1 = static_cast<int>(min(end, hi) - start);
+  g->first_cta = start >= lo && start < hi ? static_cast<int>(blockIdx.x) : static_cast<int>(start / share);
+  g->last_cta = end <= hi ? static_cast<int>(blockIdx.x) : static_cast<int>((end - 1) / share);
+}
+
+// Fills the plan; all THREADS threads call it, and meet at its end.
 template <int THREADS>
-__device__ Kv8Run kv8_run(const Kv8AttendArgs& a, const Kv8Work& w) {
+__device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan) {
   constexpr int W = THREADS / 32;
-  __shared__ int64_t sums[W + 1];
-  __shared__ int64_t found[2];
+  __shared__ int64_t sums[W];
+  __shared__ int counts[W];
+  __shared__ int before_first;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
-  int64_t mine = 0;
-  for (int64_t i = tid; i < w.items; i += THREADS) mine += kv8_item(a, w, i).steps;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-  if (lane == 0) sums[warp] = mine;
-  __syncthreads();
+  const bool one = w.items <= THREADS;  // every thread has one item at most: once is enough
   int64_t total = 0;
+  Kv8Segment g{};
+  if (one) {
+    if (tid < w.items) g.it = kv8_item(a, w, tid);
+    // a part of an item for each CTA?
+    const int parts = (g.it.steps + w.min_steps - 1) / w.min_steps;
+    int sum = parts;
 #pragma unroll
-  for (int i = 0; i < W; ++i) total += sums[i];
-  Kv8Run r;
-  r.share = max(static_cast<int64_t>(w.min_steps), (total + gridDim.x - 1) / gridDim.x);
-  r.lo = min(total, r.share * blockIdx.x);
-  r.hi = min(total, r.lo + r.share);
-  r.item = r.start = 0;
-  if (r.lo >= r.hi) return r;  // (the same for the whole CTA)
-  int64_t carry = 0;
-  for (int64_t base = 0; base < w.items; base += THREADS) {
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum = min(sum + v, 1 << 20);
+    }
+    if (lane == 31) counts[warp] = sum;
+    if (tid == 0) {
+      plan->n = 0;
+      plan->more = false;
+    }
     __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      if (j < warp) before += counts[j];
+      all += counts[j];
+    }
+    if (all <= static_cast<int>(gridDim.x)) {
+      const int first = before + sum - parts, cta = static_cast<int>(blockIdx.x);
+      if (cta >= first && cta < first + parts) {
+        g.s0 = static_cast<int>(static_cast<int64_t>(g.it.steps) * (cta - first) / parts);
+        g.s1 = static_cast<int>(static_cast<int64_t>(g.it.steps) * (cta - first + 1) / parts);
+        g.first_cta = first;
+        g.last_cta = first + parts - 1;
+        plan->seg[0] = g;
+        plan->n = 1;
+      }
+      __syncthreads();
+      return;
+    }
+    __syncthreads();
+  }
+  if (!one) {
+    int64_t mine = 0;
+    for (int64_t i = tid; i < w.items; i += THREADS) {
+      const int steps = kv8_item(a, w, i).steps;
+      mine += steps ? steps + w.item_steps : 0;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (lane == 0) sums[warp] = mine;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) total += sums[i];
+    __syncthreads();
+  }
+  if (tid == 0) {
+    plan->n = 0;
+    plan->more = false;
+  }
+  int64_t carry = 0, lo = 0, hi = 0, share = 1;
+  int carried = 0;  // segments so far
+  for (int64_t base = 0; base < w.items; base += THREADS) {
     const int64_t i = base + tid;
-    const int64_t steps = i < w.items ? kv8_item(a, w, i).steps : 0;
-    int64_t sum = steps;
+    if (!one) {
+      g.it.steps = 0;
+      if (i < w.items) g.it = kv8_item(a, w, i);
+    }
+    const int64_t cost = g.it.steps ? g.it.steps + w.item_steps : 0;
+    int64_t sum = cost;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
@@ -190,46 +265,67 @@ __device__ Kv8Run kv8_run(const Kv8AttendArgs& a, const Kv8Work& w) {
       if (j < warp) before += sums[j];
       all += sums[j];
     }
-    const int64_t end = before + sum, begin = end - steps;
-    if (r.lo >= begin && r.lo < end) {
-      found[0] = i;
-      found[1] = begin;
+    if (one) total = all;
+    share = max(static_cast<int64_t>(1), (total + gridDim.x - 1) / gridDim.x);
+    lo = min(total, share * blockIdx.x);
+    hi = min(total, lo + share);
+    const int64_t end = before + sum, start = end - g.it.steps;  // of its own steps
+    const bool mine = g.it.steps > 0 && start < hi && end > lo;
+    const uint32_t those = __ballot_sync(0xffffffffu, mine);
+    if (lane == 0) counts[warp] = __popc(those);
+    __syncthreads();
+    int at = carried + __popc(those & ((1u << lane) - 1));
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      if (j < warp) at += counts[j];
+      carried += counts[j];
+    }
+    if (mine && at < kSegments) {
+      kv8_cut(&g, start, lo, hi, share);
+      plan->seg[at] = g;
+    }
+    if (mine && at == kSegments) {
+      plan->more = true;
+      plan->more_item = i;
+      plan->more_start = start;
     }
     carry += all;
-    if (carry > r.lo) break;  // (the same for the whole CTA)
+    if (carry >= hi) break;  // (the same for the whole CTA)
+    __syncthreads();
+  }
+  if (tid == 0) {
+    plan->n = min(carried, kSegments);
+    plan->hi = hi;
+    plan->share = share;
   }
   __syncthreads();
-  r.item = found[0];
-  r.start = found[1];
-  return r;
 }
 
-// Walks over the segments of a run: every role of a CTA has a walk of its own.
+// Walks over the segments of the plan: every role of a CTA has a walk of its own.
 struct Kv8Walk {
-  int64_t at, start, item;
-  Kv8Item it;
-  int s0, s1;          // steps of the item that this CTA does
-  int64_t first_cta, last_cta;  // CTAs that the item is shared by
-  __device__ __forceinline__ explicit Kv8Walk(const Kv8Run& r) : at(r.lo), start(r.start), item(r.item) {}
-  __device__ __forceinline__ bool next(const Kv8AttendArgs& a, const Kv8Work& w, const Kv8Run& r) {
-    if (at >= r.hi) return false;
-    for (;; ++item) {
-      it = kv8_item(a, w, item);
-      if (it.steps) break;
+  int i = 0;
+  int64_t item, start;
+  Kv8Segment g;
+  __device__ __forceinline__ bool next(const Kv8AttendArgs& a, const Kv8Work& w, const Kv8Plan& plan) {
+    if (i < plan.n) {
+      g = plan.seg[i++];
+      return true;
     }
-    s0 = static_cast<int>(at - start);
-    s1 = static_cast<int>(min(static_cast<int64_t>(it.steps), r.hi - start));
-    first_cta = start / r.share;
-    last_cta = (start + it.steps - 1) / r.share;
-    at = start + s1;
-    start += it.steps;
+    if (!plan.more) return false;
+    if (i++ == kSegments) {
+      item = plan.more_item;
+      start = plan.more_start;
+    }
+    if (start >= plan.hi) return false;
+    for (;; ++item) {
+      g.it = kv8_item(a, w, item);
+      if (g.it.steps) break;
+    }
+    kv8_cut(&g, start, plan.share * blockIdx.x, plan.hi, plan.share);
+    start += g.it.steps + w.item_steps;
     ++item;
     return true;
   }
-  __device__ __forceinline__ bool whole() const { return first_cta == last_cta; }
-  // where this CTA's part of the item goes: each has at most one item that began earlier and one that goes on
-  __device__ __forceinline__ int64_t slot() const { return 2 * static_cast<int64_t>(blockIdx.x) + (s0 == 0 ? 1 : 0); }
-  __device__ __forceinline__ static int64_t slot_of(int64_t cta, int64_t first) { return 2 * cta + (cta == first ? 1 : 0); }
 };
 
 // A page of an item: its number in the pools, or -1 where there is none to be seen.

@@ -29,6 +29,8 @@ bool config_ok(const hsa_kv8_config* c) {
   if (c->page_tokens != HSA_PAGE_TOKENS) return false;
   if (c->max_pages < 1 || c->max_blocks < 1 || c->max_tokens < 1) return false;
   if (c->max_batch < 1 || c->max_batch > 4096) return false;
+  // items of an attention launch: (sequence, key head, 8 rows or more)
+  if ((static_cast<int64_t>(c->max_tokens) * (c->num_heads / c->num_kv_heads) / 8 + 1) * c->max_batch * c->num_kv_heads >= (1ll << 31)) return false;
   if (static_cast<int64_t>(c->max_pages) * c->num_kv_heads * kBlock >= (1ll << 31)) return false;  // rows of a pool: TMA coordinates
   if (static_cast<int64_t>(c->max_blocks) * kBlock >= (1ll << 31)) return false;                   // lengths are int32
   if (!(c->softmax_scale >= 0.f) || !std::isfinite(c->softmax_scale)) return false;

@@ -17,7 +17,10 @@
 // fp32, while the next step's products run.  (Summed over pages on the tensor core, the weights would have to carry the
 // scales, and one page with a large value would cost the weights of all others their low bits.)
 //
-// Warps: 0 loads pages, 1 issues products, 2 and 3 prepare the rows of Q of the next item, 4 to 7 softmax and output.
+// Warps: 0 loads pages, 1 issues the first products and 3 the second ones (one thread for both spends 1600 cycles a step on
+// looking at barriers and issuing, the loads of a step take 1400), 2 prepares the rows of Q of the next item, then one or two
+// groups of four for softmax and output.  Two groups take the steps in turn, each with sums and references of its own, which they bring
+// together at an item's end; the group that had the item's last step writes it, while the other goes on.
 #include <cuda_fp8.h>
 #include <cuda_fp16.h>
 
@@ -28,7 +31,6 @@ namespace hsa {
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr float kShift = 7.f;   // the largest weight is 2^7 when the reference is set ...
 constexpr float kSlack = 1.75f; // ... and may grow to 2^8.75 < 448 before it is set anew
 constexpr float kNone = -1e30f; // reference of a row that has seen nothing
@@ -38,19 +40,18 @@ struct PageMeta {
   float ks, vs; // scales; vs 0: no page
 };
 
-// R: rows of an item; T: tiles of 128 keys of a step
+// R: rows of an item.  A step is a tile of 128 keys, two pages.
 template <int D, int R>
 struct DecodeShape {
-  static constexpr int T = R <= 16 ? 2 : 1;
-  static constexpr int N = 2 * R;
-  static constexpr int kPages = 2 * T;                   // pages of a step
+  static constexpr int N = R < 8 ? 16 : 2 * R;           // columns of the products: first terms, then second ones (16 at least)
+  static constexpr int kGroups = R <= 16 ? 2 : 1;        // (32 rows: the registers of four warps)
+  static constexpr int kThreads = 128 + 128 * kGroups;
   static constexpr int kPage = kBlock * D;               // bytes of a page tile
-  static constexpr int kStage = kPages * kPage;          // of K or of V of a step
-  static constexpr int kStages = (R == 32 ? 5 : 3) * (D == 64 ? 2 : 1);
+  static constexpr int kStage = 2 * kPage;               // of K or of V of a step
+  static constexpr int kStages = (R == 32 ? 5 : 6) * (D == 64 ? 2 : 1);
   static constexpr uint32_t kS = 0;                      // TMEM columns: S of two steps, then O of their pages
-  static constexpr uint32_t kO = 2 * T * N;
-  static constexpr uint32_t kCols = kO + 2 * kPages * N <= 256 ? 256 : 512;
-  static_assert(kO + 2 * kPages * N <= 512, "");
+  static constexpr uint32_t kO = 2 * N;
+  static constexpr uint32_t kCols = 6 * N <= 128 ? 128 : 6 * N <= 256 ? 256 : 512;
 };
 
 template <int D, int R>
@@ -58,16 +59,17 @@ struct DecodeSmem {
   using Sh = DecodeShape<D, R>;
   uint8_t k[Sh::kStages][Sh::kStage];
   uint8_t v[Sh::kStages][Sh::kStage];
-  uint8_t p[2][Sh::T][Sh::N * 128];        // weights: [hi rows | lo rows][128 keys]
+  uint8_t p[2][Sh::N * 128];               // weights: [hi rows | lo rows][128 keys]
   uint8_t q[2][Sh::N * D];
+  float other[Sh::kGroups == 2 ? R * (D + 2) : 1];  // sums of the group that does not write the item: [R][D], references, sums of weights
   float qscale[2][R];
-  PageMeta meta[Sh::kStages][Sh::kPages];
-  float red[4][R];
-  float lsum[4][R];
+  PageMeta meta[Sh::kStages][2];
+  float red[Sh::kGroups][4][R];
   uint64_t k_full[Sh::kStages], v_full[Sh::kStages], empty[Sh::kStages];
-  uint64_t s_full[2], s_free[2], p_full[2], p_free[2], q_full[2], q_free[2], done;
+  uint64_t s_full[2], s_free[2], p_full[2], p_free[2], q_full[2], q_free[2], other_full, other_free, done[2];
   uint32_t tmem;
   int last;
+  Kv8Plan plan;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -75,20 +77,31 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ bool softmax_any(bool x) {
+// the bytes alone: the arrival comes later
+__device__ __forceinline__ void mbar_expect_tx_only(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+// The four warps of a group meet; `any`: whether x holds for one of them.
+__device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + group) : "memory"); }
+__device__ __forceinline__ bool group_any(int group, bool x) {
   uint32_t r;
   asm volatile(
       "{\n"
       ".reg .pred p, q;\n"
-      "setp.ne.u32 p, %1, 0;\n"
-      "barrier.cta.red.or.pred q, 2, 128, p;\n"
+      "setp.ne.u32 p, %2, 0;\n"
+      "barrier.cta.red.or.pred q, %1, 128, p;\n"
       "selp.u32 %0, 1, 0, q;\n"
       "}\n"
       : "=r"(r)
-      : "r"(static_cast<uint32_t>(x))
+      : "r"(1 + group), "r"(static_cast<uint32_t>(x))
       : "memory");
   return r != 0;
+}
+
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -139,13 +152,65 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r) {
   }
 }
 
+// Adds the parts of an item up, in the order of the CTAs, and writes its rows: 128 threads, four dims of a row at a time.
 template <int D, int R>
-__global__ void __launch_bounds__(kThreads, 1) kv8_decode_kernel(const Kv8AttendArgs a, const Kv8Work w,
-                                                                 const __grid_constant__ CUtensorMap tm_k,
-                                                                 const __grid_constant__ CUtensorMap tm_v) {
+__device__ __forceinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w, const Kv8Segment& g, int tid) {
+  constexpr int F = D / 4, kAtOnce = 8;
+  for (int i = tid; i < g.it.rows * F; i += 128) {
+    const int r = i / F, f = i % F;
+    float m = kNone, tot = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = g.first_cta; c0 <= g.last_cta; c0 += kAtOnce) {
+      float pm[kAtOnce], pl[kAtOnce];
+      float4 pv[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        pm[j] = kNone;
+        pl[j] = 0.f;
+        pv[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c0 + j <= g.last_cta) {
+          const float* p = w.parts + Kv8Segment::slot_of(c0 + j, g.first_cta) * w.slot_floats;
+          pm[j] = __ldcg(p + R * D + r);
+          pl[j] = __ldcg(p + R * D + R + r);
+          pv[j] = __ldcg(reinterpret_cast<const float4*>(p + r * D + f * 4));
+        }
+      }
+      float to = m;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) to = fmaxf(to, pm[j]);
+      const float c = ex2(m - to);
+      m = to;
+      sum.x *= c;
+      sum.y *= c;
+      sum.z *= c;
+      sum.w *= c;
+      tot *= c;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const float k = ex2(pm[j] - to);
+        sum.x = fmaf(pv[j].x, k, sum.x);
+        sum.y = fmaf(pv[j].y, k, sum.y);
+        sum.z = fmaf(pv[j].z, k, sum.z);
+        sum.w = fmaf(pv[j].w, k, sum.w);
+        tot = fmaf(pl[j], k, tot);
+      }
+    }
+    const int at = g.it.row0 + r;
+    const int64_t tok = g.it.first + at / a.group;
+    const int head = g.it.h * a.group + at % a.group;
+    const float down = tot == 0.f ? 0.f : 1.f / tot;
+    *reinterpret_cast<uint2*>(a.out + tok * a.ots + head * a.ohs + f * 4) =
+        make_uint2(pack_bf16(sum.x * down, sum.y * down), pack_bf16(sum.z * down, sum.w * down));
+    if (a.lse && f == 0) a.lse[tok * a.Hq + head] = tot == 0.f ? -INFINITY : (m - kShift + log2f(tot)) * 0.69314718055994531f;
+  }
+}
+
+template <int D, int R>
+__global__ void __launch_bounds__((DecodeShape<D, R>::kThreads), 1)
+kv8_decode_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using Sh = DecodeShape<D, R>;
   using Smem = DecodeSmem<D, R>;
-  constexpr int T = Sh::T, N = Sh::N, kPages = Sh::kPages, kStages = Sh::kStages;
+  constexpr int N = Sh::N, kStages = Sh::kStages, kGroups = Sh::kGroups;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
@@ -160,10 +225,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_decode_kernel(const Kv8Attend
       mbar_init(&sm.s_free[i], 128);
       mbar_init(&sm.p_full[i], 128);
       mbar_init(&sm.p_free[i], 1);
-      mbar_init(&sm.q_full[i], 64);
-      mbar_init(&sm.q_free[i], 5);  // its products, and the softmax warps (its scales)
+      mbar_init(&sm.done[i], 1);
+      mbar_init(&sm.q_full[i], 32);
+      mbar_init(&sm.q_free[i], 1 + 4 * kGroups);  // its products, and the softmax warps (its scales)
     }
-    mbar_init(&sm.done, 1);
+    mbar_init(&sm.other_full, 128);
+    mbar_init(&sm.other_free, 128);
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -174,12 +241,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_decode_kernel(const Kv8Attend
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const Kv8Run run = kv8_run<kThreads>(a, w);
+  kv8_plan<Sh::kThreads>(a, w, &sm.plan);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
-  Kv8Walk walk(run);
+  Kv8Walk walk;
   bool ok = true;  // false: a wait ran out; nothing more is waited for
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
     if (ok && !mbar_wait(bar, parity)) {
@@ -192,47 +259,49 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_decode_kernel(const Kv8Attend
   const auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
 
   if (warp == 0) {
-    // ---- loads.  The lanes look up the pages of some steps at once.
-    constexpr int kLook = 32 / kPages;
+    // ---- loads.  The lanes look up the pages of 16 steps at once.
     uint32_t n = 0;
-    while (ok && walk.next(a, w, run)) {
-      const Kv8Item& it = walk.it;
-      for (int s = walk.s0; s < walk.s1 && ok; s += kLook) {
+    while (ok && walk.next(a, w, sm.plan)) {
+      const Kv8Item& it = walk.g.it;
+      for (int s = walk.g.s0; s < walk.g.s1 && ok; s += 16) {
         int blk = 0, page = -1;
         PageMeta meta{-1, 0.f, 0.f};
-        if (s + lane / kPages < walk.s1) page = kv8_page(a, it, s * kPages + lane, &blk);
+        if (s + lane / 2 < walk.g.s1) page = kv8_page(a, it, s * 2 + lane, &blk);
         if (page >= 0) {
           const int64_t ph = static_cast<int64_t>(page) * a.Hkv + it.h;
           meta.pos = blk * kBlock;
           meta.ks = __ldg(a.k_scale + ph);
           meta.vs = __ldg(a.v_scale + ph);
         }
-        const int count = min(kLook, walk.s1 - s);
+        const int count = min(16, walk.g.s1 - s);
         for (int i = 0; i < count; ++i, ++n) {
           const uint32_t st = n % kStages;
           if (!warp_wait(&sm.empty[st], ((n / kStages) & 1) ^ 1)) break;
-          if (lane / kPages == i) sm.meta[st][lane % kPages] = meta;
-          int pages[kPages], bytes = 0;
+          int pages[2], bytes = 0;
 #pragma unroll
-          for (int j = 0; j < kPages; ++j) {
-            pages[j] = __shfl_sync(0xffffffffu, page, i * kPages + j);
+          for (int j = 0; j < 2; ++j) {
+            pages[j] = __shfl_sync(0xffffffffu, page, i * 2 + j);
             if (pages[j] >= 0) bytes += Sh::kPage;
           }
-          __syncwarp();
+          // the loads go out before the scales are there; the keys' barrier is arrived at behind them
           if (elect_one_sync()) {
+            if (bytes) mbar_expect_tx_only(&sm.k_full[st], bytes);
 #pragma unroll
-            for (int which = 0; which < 2; ++which) {
-              uint64_t* full = which ? &sm.v_full[st] : &sm.k_full[st];
-              if (bytes) mbar_expect_tx(full, bytes);
-              else mbar_arrive(full);
+            for (int j = 0; j < 2; ++j)
+              if (pages[j] >= 0)
+                tma_load_2d(sm.k[st] + j * Sh::kPage, &tm_k, &sm.k_full[st], 0,
+                            static_cast<int>((static_cast<int64_t>(pages[j]) * a.Hkv + it.h) * kBlock));
+            if (bytes) mbar_expect_tx(&sm.v_full[st], bytes);
+            else mbar_arrive(&sm.v_full[st]);
 #pragma unroll
-              for (int j = 0; j < kPages; ++j)
-                if (pages[j] >= 0)
-                  tma_load_2d((which ? sm.v[st] : sm.k[st]) + j * Sh::kPage, which ? &tm_v : &tm_k, full, 0,
-                              static_cast<int>((static_cast<int64_t>(pages[j]) * a.Hkv + it.h) * kBlock));
-            }
+            for (int j = 0; j < 2; ++j)
+              if (pages[j] >= 0)
+                tma_load_2d(sm.v[st] + j * Sh::kPage, &tm_v, &sm.v_full[st], 0,
+                            static_cast<int>((static_cast<int64_t>(pages[j]) * a.Hkv + it.h) * kBlock));
           }
+          if (lane / 2 == i) sm.meta[st][lane % 2] = meta;
           __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.k_full[st]);
         }
       }
     }
@@ -242,296 +311,327 @@ __global__ void __launch_bounds__(kThreads, 1) kv8_decode_kernel(const Kv8Attend
         mbar_wait(&sm.v_full[(n - i) % kStages], ((n - i) / kStages) & 1);
       }
   } else if (warp == 1) {
-    // ---- products
+    // ---- first products
     if (elect_one_sync()) {
-      constexpr uint32_t id_s = idesc_e4m3(128, N, 0, 0), id_o = idesc_e4m3(128, N, 1, 0);
-      const uint32_t k0 = smem_u32(sm.k), v0 = smem_u32(sm.v), p0 = smem_u32(sm.p), q0 = smem_u32(sm.q);
-      uint32_t n = 0, items = 0;      // steps and items so far
-      int pending = -1;               // pages of the step whose second product is still to come; bit j: page j is there
-      // The second product of step n - 1.
-      const auto second = [&]() {
-        const uint32_t j = n - 1, st = j % kStages, b = j & 1;
-        if (!wait(&sm.p_full[b], (j / 2) & 1) || !wait(&sm.v_full[st], (j / kStages) & 1)) return;
-        tc_fence_after();
-#pragma unroll
-        for (int pg = 0; pg < kPages; ++pg)
-          if (pending & (1 << pg)) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              // 32 keys: rows of V, bytes of a row of P.  (head_dim 64: the upper half of M reads what lies a page further,
-              // whatever that is; those lanes of the accumulator are not looked at.)
-              const uint64_t da = row_desc<D>(v0 + st * Sh::kStage + pg * Sh::kPage + half * 32 * D, D == 128 ? 0 : Sh::kPage);
-              const uint64_t db = row_desc<128>(p0 + (b * T + pg / 2) * (N * 128) + (pg & 1) * 64 + half * 32, 0);
-              mma_f8(tmem + Sh::kO + (b * kPages + pg) * N, da, db, id_o, half);
-            }
-          }
-        tc_commit(&sm.empty[st]);
-        tc_commit(&sm.p_free[b]);
-      };
-      while (ok && walk.next(a, w, run)) {
+      constexpr uint32_t id = idesc_e4m3(128, N, 0, 0);
+      const uint64_t k0 = row_desc<D>(smem_u32(sm.k), 0), q0 = row_desc<D>(smem_u32(sm.q), 0);
+      uint32_t n = 0, items = 0, st = 0, round = 0;
+      while (ok && walk.next(a, w, sm.plan)) {
         const uint32_t qb = items & 1;
         if (!wait(&sm.q_full[qb], (items / 2) & 1)) break;
-        for (int s = walk.s0; s < walk.s1 && ok; ++s) {
-          const uint32_t st = n % kStages, b = n & 1;
-          if (!wait(&sm.k_full[st], (n / kStages) & 1) || !wait(&sm.s_free[b], ((n / 2) & 1) ^ 1)) break;
+        for (int s = walk.g.s0; s < walk.g.s1; ++s, ++n) {
+          const uint32_t b = n & 1;
+          if (!wait(&sm.k_full[st], round & 1) || !wait(&sm.s_free[b], ((n / 2) & 1) ^ 1)) break;
           tc_fence_after();
-          int there = 0;
 #pragma unroll
-          for (int pg = 0; pg < kPages; ++pg) there |= (sm.meta[st][pg].pos >= 0 ? 1 : 0) << pg;
-#pragma unroll
-          for (int tt = 0; tt < T; ++tt)
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk)
-              mma_f8(tmem + Sh::kS + (b * T + tt) * N, row_desc<D>(k0 + st * Sh::kStage + tt * 2 * Sh::kPage + kk * 32, 0),
-                     row_desc<D>(q0 + qb * (N * D) + kk * 32, 0), id_s, kk > 0);
+          for (int kk = 0; kk < D / 32; ++kk)  // (descriptors count in 16 bytes)
+            mma_f8(tmem + Sh::kS + b * N, k0 + (st * Sh::kStage + kk * 32) / 16, q0 + (qb * (N * D) + kk * 32) / 16, id, kk > 0);
           tc_commit(&sm.s_full[b]);
-          if (s == walk.s1 - 1) tc_commit(&sm.q_free[qb]);
-          if (pending >= 0) second();
-          pending = there;
-          ++n;
+          if (s == walk.g.s1 - 1) tc_commit(&sm.q_free[qb]);
+          if (++st == kStages) {
+            st = 0;
+            ++round;
+          }
         }
         ++items;
       }
-      if (ok && pending >= 0) second();
-      tc_commit(&sm.done);
-      mbar_wait(&sm.done, 0);
+      tc_commit(&sm.done[0]);
+      mbar_wait(&sm.done[0], 0);
     }
     __syncwarp();
-  } else if (warp < 4) {
-    // ---- rows of Q, an item ahead: a warp takes every other row
-    uint32_t items = 0;
-    while (ok && walk.next(a, w, run)) {
-      const Kv8Item& it = walk.it;
-      const uint32_t qb = items & 1;
-      if (!warp_wait(&sm.q_free[qb], ((items / 2) & 1) ^ 1)) break;
-      constexpr int PER = D / 32;
-#pragma unroll 4
-      for (int r = warp & 1; r < R; r += 2) {
-        float x[PER];
-        float top = 0.f;
+  } else if (warp == 3) {
+    // ---- second products, a page at a time
+    if (elect_one_sync()) {
+      constexpr uint32_t id = idesc_e4m3(128, N, 1, 0);
+      // (head_dim 64: the upper half of M reads what lies a page further, whatever that is; those lanes of the accumulator
+      // are not looked at)
+      const uint64_t v0 = row_desc<D>(smem_u32(sm.v), D == 128 ? 0 : Sh::kPage), p0 = row_desc<128>(smem_u32(sm.p), 0);
+      uint32_t n = 0, st = 0, round = 0;
+      while (ok && walk.next(a, w, sm.plan)) {
+        for (int s = walk.g.s0; s < walk.g.s1; ++s, ++n) {
+          const uint32_t b = n & 1;
+          if (!wait(&sm.p_full[b], (n / 2) & 1) || !wait(&sm.v_full[st], round & 1)) break;
+          tc_fence_after();
 #pragma unroll
-        for (int j = 0; j < PER; ++j) x[j] = 0.f;
-        if (r < it.rows) {
-          const int at = it.row0 + r;
-          const __nv_bfloat16* src = a.q + (it.first + at / a.group) * a.ts + (it.h * a.group + at % a.group) * a.hs + lane * PER;
+          for (int pg = 0; pg < 2; ++pg)
+            if (sm.meta[st][pg].pos >= 0) {
 #pragma unroll
-          for (int j = 0; j < PER; ++j) {
-            x[j] = __bfloat162float(src[j]);
-            if (fabsf(x[j]) < INFINITY) top = fmaxf(top, fabsf(x[j]));
+              for (int half = 0; half < 2; ++half)  // 32 keys: rows of V, bytes of a row of P
+                mma_f8(tmem + Sh::kO + (b * 2 + pg) * N, v0 + (st * Sh::kStage + pg * Sh::kPage + half * 32 * D) / 16,
+                       p0 + (b * (N * 128) + pg * 64 + half * 32) / 16, id, half);
+            }
+          tc_commit(&sm.empty[st]);
+          tc_commit(&sm.p_free[b]);
+          if (++st == kStages) {
+            st = 0;
+            ++round;
           }
         }
+      }
+      tc_commit(&sm.done[1]);
+      mbar_wait(&sm.done[1], 0);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // ---- rows of Q, an item ahead: a thread takes 8 dims of a row
+    uint32_t items = 0;
+    while (ok && walk.next(a, w, sm.plan)) {
+      const Kv8Item& it = walk.g.it;
+      const uint32_t qb = items & 1;
+      constexpr int V = D / 8, kRows = 32 / V;     // vectors of a row, rows at a time
+      constexpr int kTimes = (R + kRows - 1) / kRows;
+      const int r0 = lane / V, c = lane % V;
+      uint4 in[kTimes];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      for (int i = 0; i < kTimes; ++i) {
+        const int r = r0 + i * kRows;
+        in[i] = make_uint4(0, 0, 0, 0);
+        if (r < it.rows) {
+          const int at = it.row0 + r;
+          in[i] = __ldg(reinterpret_cast<const uint4*>(a.q + (it.first + at / a.group) * a.ts + (it.h * a.group + at % a.group) * a.hs + c * 8));
+        }
+      }
+      if (!warp_wait(&sm.q_free[qb], ((items / 2) & 1) ^ 1)) break;
+      uint8_t* q = sm.q[qb];
+#pragma unroll
+      for (int i = 0; i < kTimes; ++i) {
+        const int r = r0 + i * kRows;
+        const uint32_t words[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
+        float x[8];
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[j] = __uint_as_float(j & 1 ? words[j / 2] & 0xffff0000u : words[j / 2] << 16);
+          // (what is not finite: NaN, which spoils the row and no other)
+          if (fabsf(x[j]) < INFINITY) top = fmaxf(top, fabsf(x[j]));
+          else x[j] = NAN;
+        }
+#pragma unroll
+        for (int o = V / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const int e = max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100) - 7;  // (rows of zeros: any will do)
         const float up = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-        uint8_t* q = sm.q[qb];
+        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int j = 0; j < PER; j += 2) {
-          // (what is not finite: NaN, which spoils the row and no other)
-          const float c0 = fabsf(x[j]) < INFINITY ? x[j] * up : NAN, c1 = fabsf(x[j + 1]) < INFINITY ? x[j + 1] * up : NAN;
-          uint32_t hi, lo;
-          two_terms(c0, c1, &hi, &lo);
-          *reinterpret_cast<uint16_t*>(q + swizzled<D>(r, lane * PER + j)) = static_cast<uint16_t>(hi);
-          *reinterpret_cast<uint16_t*>(q + swizzled<D>(R + r, lane * PER + j)) = static_cast<uint16_t>(lo);
+        for (int j = 0; j < 4; ++j) two_terms(x[2 * j] * up, x[2 * j + 1] * up, &hi[j], &lo[j]);
+        if (R % kRows == 0 || r < R) {
+          *reinterpret_cast<uint2*>(q + swizzled<D>(r, c * 8)) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+          *reinterpret_cast<uint2*>(q + swizzled<D>(N / 2 + r, c * 8)) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+          if (c == 0) sm.qscale[qb][r] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * a.scale_log2;
         }
-        if (lane == 0) sm.qscale[qb][r] = __uint_as_float(static_cast<uint32_t>(127 + e) << 23) * a.scale_log2;
       }
       fence_proxy_async_smem();
       mbar_arrive(&sm.q_full[qb]);
       ++items;
     }
   } else {
-    // ---- softmax: a thread is a key of each tile, and a dim of the output.  After a wait that ran out the threads go on
+    // ---- softmax: a thread is a key of the tile, and a dim of the output.  After a wait that ran out the threads go on
     // with whatever is there, because they meet at barriers; the status word says that the result is none.
+    const int group = kGroups == 2 ? (warp - 4) / 4 : 0;
     const int w4 = warp & 3, key = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
-    uint32_t n = 0, items = 0;
-    while (walk.next(a, w, run)) {
-      const Kv8Item& it = walk.it;
+    uint32_t n = 0, items = 0, merges = 0;
+    Kv8Segment shared[2];
+    int n_shared = 0;
+    while (walk.next(a, w, sm.plan)) {
+      const Kv8Item& it = walk.g.it;
+      const int steps = walk.g.s1 - walk.g.s0;
       const uint32_t qb = items & 1;
-      wait(&sm.q_full[qb], (items / 2) & 1);
+      ++items;
+      // steps n, n + 1, ... are this item's; every kGroups-th one is this group's
+      uint32_t j = n + (kGroups == 2 ? (n + group) & 1 : 0);
+      const uint32_t end = n + steps;
+      n = end;
+      const bool writes = kGroups == 1 || ((end - 1) & 1) == static_cast<uint32_t>(group);
+      const bool both = kGroups == 2 && steps > 1;
       float ref[R], l[R], o[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         ref[r] = kNone;
         l[r] = o[r] = 0.f;
       }
-      const int lim_low = it.limit(a, 0);
-      float vs[kPages];       // of the step whose second product has not been added yet
-      bool pending = false;
-      // adds what the second product of step j gave
-      const auto add = [&](uint32_t j) {
-        wait(&sm.p_free[j & 1], (j / 2) & 1);
+      const int lim_low = it.limit(a, 0), rows = it.rows;
+      float vs0 = 0.f, vs1 = 0.f;       // scales of the step whose second product has not been added yet
+      uint32_t added = j;               // steps up to here have been
+      // adds what the second product of step i gave
+      const auto add = [&](uint32_t i) {
+        wait(&sm.p_free[i & 1], (i / 2) & 1);
         __syncwarp();
         tc_fence_after();
 #pragma unroll
-        for (int pg = 0; pg < kPages; ++pg)
-          if (vs[pg] > 0.f) {
+        for (int pg = 0; pg < 2; ++pg) {
+          const float vs = pg ? vs1 : vs0;
+          if (vs > 0.f) {
             uint32_t x[N];
-            tmem_load<N>(tmem + lanes + Sh::kO + ((j & 1) * kPages + pg) * N, x);
+            tmem_load<N>(tmem + lanes + Sh::kO + ((i & 1) * 2 + pg) * N, x);
             tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < R; ++r) o[r] = fmaf(fmaf(__uint_as_float(x[R + r]), kLow, __uint_as_float(x[r])), vs[pg], o[r]);
+            for (int r = 0; r < R; ++r) o[r] = fmaf(fmaf(__uint_as_float(x[N / 2 + r]), kLow, __uint_as_float(x[r])), vs, o[r]);
           }
+        }
         tc_fence_before();
-        pending = false;
+        added = i + kGroups;
       };
-      for (int s = walk.s0; s < walk.s1; ++s, ++n) {
-        const uint32_t st = n % kStages, b = n & 1;
-        wait(&sm.k_full[st], (n / kStages) & 1);  // (long since: for the pages' scales)
-        wait(&sm.s_full[b], (n / 2) & 1);
+      wait(&sm.q_full[qb], ((items - 1) / 2) & 1);
+      for (; j < end; j += kGroups) {
+        const uint32_t st = j % kStages, b = j & 1;
+        wait(&sm.s_full[b], (j / 2) & 1);
         __syncwarp();
         tc_fence_after();
-        float y[T][R];
+        float y[R];
         bool over = false;
-#pragma unroll
-        for (int tt = 0; tt < T; ++tt) {
+        {
           uint32_t x[N];
-          tmem_load<N>(tmem + lanes + Sh::kS + (b * T + tt) * N, x);
-          const PageMeta meta = sm.meta[st][tt * 2 + key / kBlock];
+          tmem_load<N>(tmem + lanes + Sh::kS + b * N, x);
+          const PageMeta meta = sm.meta[st][key / kBlock];
           const int pos = meta.pos + key % kBlock;
           tc_wait_ld();
 #pragma unroll
-          for (int r = 0; r < R; ++r) y[tt][r] = fmaf(__uint_as_float(x[R + r]), kLow, __uint_as_float(x[r])) * (sm.qscale[qb][r] * meta.ks);
+          for (int r = 0; r < R; ++r) y[r] = fmaf(__uint_as_float(x[N / 2 + r]), kLow, __uint_as_float(x[r])) * (sm.qscale[qb][r] * meta.ks);
           if (meta.pos < 0) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) y[tt][r] = -INFINITY;
+            for (int r = 0; r < R; ++r) y[r] = -INFINITY;
           } else if (pos >= lim_low) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
-              if (pos >= it.limit(a, min(r, it.rows - 1))) y[tt][r] = -INFINITY;
+              if (pos >= it.limit(a, min(r, rows - 1))) y[r] = -INFINITY;
           }
 #pragma unroll
-          for (int r = 0; r < R; ++r) over |= y[tt][r] > ref[r] + kSlack;
+          for (int r = 0; r < R; ++r) over |= y[r] > ref[r] + kSlack;
         }
-        float vs_now[kPages];
-#pragma unroll
-        for (int pg = 0; pg < kPages; ++pg) vs_now[pg] = sm.meta[st][pg].vs;
+        const float vs0_now = sm.meta[st][0].vs, vs1_now = sm.meta[st][1].vs;
         tc_fence_before();
         mbar_arrive(&sm.s_free[b]);
-        if (softmax_any(over)) {
+        if (group_any(group, over)) {
           // the maxima anew
-          if (pending) add(n - 1);
+          if (added < j) add(added);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            float top = y[0][r];
-#pragma unroll
-            for (int tt = 1; tt < T; ++tt) top = fmaxf(top, y[tt][r]);
-#pragma unroll
-            for (int o2 = 16; o2 > 0; o2 >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o2));
-            if (lane == 0) sm.red[w4][r] = top;
+            const float top = warp_max(y[r]);
+            if (lane == 0) sm.red[group][w4][r] = top;
           }
-          softmax_sync();
+          group_sync(group);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            const float top = fmaxf(fmaxf(sm.red[0][r], sm.red[1][r]), fmaxf(sm.red[2][r], sm.red[3][r]));
+            const float* red = &sm.red[group][0][r];
+            const float top = fmaxf(fmaxf(red[0], red[R]), fmaxf(red[2 * R], red[3 * R]));
             const float to = top > ref[r] + kSlack ? top : ref[r], c = ex2(ref[r] - to);
             ref[r] = to;
             l[r] *= c;
             o[r] *= c;
           }
-          softmax_sync();  // (red is free again)
+          group_sync(group);  // (red is free again)
         }
-        // (the buffer of P: what it held two steps ago has been added)
+        // (the buffer of P: what it held two steps ago has been multiplied before that could be added)
+        if (kGroups == 2 && added < j) add(added);
+        uint8_t* p = sm.p[b];
 #pragma unroll
-        for (int tt = 0; tt < T; ++tt) {
-          uint8_t* p = sm.p[b][tt];
-#pragma unroll
-          for (int r = 0; r < R; r += 2) {
-            const float p0 = ex2(y[tt][r] + (kShift - ref[r])), p1 = ex2(y[tt][r + 1] + (kShift - ref[r + 1]));
-            l[r] += p0;
-            l[r + 1] += p1;
-            uint32_t hi, lo;
-            two_terms(p0, p1, &hi, &lo);
-            p[swizzled<128>(r, key)] = static_cast<uint8_t>(hi);
-            p[swizzled<128>(r + 1, key)] = static_cast<uint8_t>(hi >> 8);
-            p[swizzled<128>(R + r, key)] = static_cast<uint8_t>(lo);
-            p[swizzled<128>(R + r + 1, key)] = static_cast<uint8_t>(lo >> 8);
-          }
+        for (int r = 0; r < R; r += 2) {
+          const float p0 = ex2(y[r] + (kShift - ref[r])), p1 = ex2(y[r + 1] + (kShift - ref[r + 1]));
+          l[r] += p0;
+          l[r + 1] += p1;
+          uint32_t hi, lo;
+          two_terms(p0, p1, &hi, &lo);
+          p[swizzled<128>(r, key)] = static_cast<uint8_t>(hi);
+          p[swizzled<128>(r + 1, key)] = static_cast<uint8_t>(hi >> 8);
+          p[swizzled<128>(N / 2 + r, key)] = static_cast<uint8_t>(lo);
+          p[swizzled<128>(N / 2 + r + 1, key)] = static_cast<uint8_t>(lo >> 8);
         }
         fence_proxy_async_smem();
         mbar_arrive(&sm.p_full[b]);
-        if (pending) add(n - 1);
-#pragma unroll
-        for (int pg = 0; pg < kPages; ++pg) vs[pg] = vs_now[pg];
-        pending = true;
+        if (added < j) add(added);
+        vs0 = vs0_now;
+        vs1 = vs1_now;
       }
-      ++items;
-
-      // ---- output: the sums of weights over the keys, then a dim of every row
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], o);
-        if (lane == 0) sm.lsum[w4][r] = l[r];
-      }
-      add(n - 1);
-      softmax_sync();
-      const bool whole = walk.whole();
-      float* part = w.parts + walk.slot() * w.slot_floats;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (r < it.rows && ok) {
-          const float sum = (sm.lsum[0][r] + sm.lsum[1][r]) + (sm.lsum[2][r] + sm.lsum[3][r]);
-          if (whole) {
-            const int at = it.row0 + r;
-            const int64_t tok = it.first + at / a.group;
-            const int head = it.h * a.group + at % a.group;
-            if (key < D) a.out[tok * a.ots + head * a.ohs + key] = __float2bfloat16_rn(sum == 0.f ? 0.f : o[r] / sum);
-            if (a.lse && key == 0) a.lse[tok * a.Hq + head] = sum == 0.f ? -INFINITY : (ref[r] - kShift + log2f(sum)) * 0.69314718055994531f;
-          } else {
-            if (key < D) part[r * D + key] = o[r];
-            if (key == 0) {
-              part[R * D + r] = ref[r];
-              part[R * D + R + r] = sum;
-            }
-          }
-        }
-      }
-      if (!whole) {
-        // the last CTA of the item to get here joins all parts
-        __threadfence();
-        softmax_sync();
-        if (key == 0) {
-          const int32_t others = static_cast<int32_t>(walk.last_cta - walk.first_cta);
-          sm.last = ok && atomicAdd(w.tickets + walk.first_cta, 1) == others;
-          __threadfence();
-          if (sm.last) w.tickets[walk.first_cta] = 0;
-        }
-        softmax_sync();
-        if (sm.last) {
-          constexpr int F = D / 4;
-          for (int i = key; i < it.rows * F; i += 128) {
-            const int r = i / F, f = i % F;
-            float m = kNone;
-#pragma unroll 4
-            for (int64_t c = walk.first_cta; c <= walk.last_cta; ++c)
-              m = fmaxf(m, __ldcg(w.parts + Kv8Walk::slot_of(c, walk.first_cta) * w.slot_floats + R * D + r));
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            float tot = 0.f;
-#pragma unroll 4
-            for (int64_t c = walk.first_cta; c <= walk.last_cta; ++c) {
-              const float* p = w.parts + Kv8Walk::slot_of(c, walk.first_cta) * w.slot_floats;
-              const float k = ex2(__ldcg(p + R * D + r) - m);
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(p + r * D + f * 4));
-              sum.x = fmaf(v.x, k, sum.x);
-              sum.y = fmaf(v.y, k, sum.y);
-              sum.z = fmaf(v.z, k, sum.z);
-              sum.w = fmaf(v.w, k, sum.w);
-              tot = fmaf(__ldcg(p + R * D + R + r), k, tot);
-            }
-            const int at = it.row0 + r;
-            const int64_t tok = it.first + at / a.group;
-            const int head = it.h * a.group + at % a.group;
-            const float down = tot == 0.f ? 0.f : 1.f / tot;
-            *reinterpret_cast<uint2*>(a.out + tok * a.ots + head * a.ohs + f * 4) =
-                make_uint2(pack_bf16(sum.x * down, sum.y * down), pack_bf16(sum.z * down, sum.w * down));
-            if (a.lse && f == 0) a.lse[tok * a.Hq + head] = tot == 0.f ? -INFINITY : (m - kShift + log2f(tot)) * 0.69314718055994531f;
-          }
-        }
-      }
-      softmax_sync();  // (lsum and last are free again)
       if (lane == 0) mbar_arrive(&sm.q_free[qb]);
+      if (!writes && !both) continue;  // the item's one step was the other group's
+
+      // ---- the item's sums: of weights over the keys, then a dim of every row
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], s);
+        if (lane == 0) sm.red[group][w4][r] = l[r];
+      }
+      add(added);
+      group_sync(group);
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float* red = &sm.red[group][0][r];
+        l[r] = (red[0] + red[R]) + (red[2 * R] + red[3 * R]);
+      }
+      if (both) {
+        if (!writes) {
+          wait(&sm.other_free, (merges & 1) ^ 1);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            if (key < D) sm.other[r * D + key] = o[r];
+            if (key == r) {
+              sm.other[R * D + r] = ref[r];
+              sm.other[R * D + R + r] = l[r];
+            }
+          }
+          mbar_arrive(&sm.other_full);
+        } else {
+          wait(&sm.other_full, merges & 1);
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const float m = sm.other[R * D + r], to = fmaxf(ref[r], m), c = ex2(ref[r] - to), k = ex2(m - to);
+            o[r] *= c;
+            if (key < D) o[r] = fmaf(sm.other[r * D + key], k, o[r]);
+            l[r] = fmaf(sm.other[R * D + R + r], k, l[r] * c);
+            ref[r] = to;
+          }
+          mbar_arrive(&sm.other_free);
+        }
+        ++merges;
+      }
+      if (writes) {
+        const bool whole = walk.g.whole();
+        float* part = w.parts + walk.g.slot() * w.slot_floats;
+        int tok = it.first + it.row0 / a.group, head = it.row0 % a.group;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          if (r < rows && ok) {
+            if (whole) {
+              const int h = it.h * a.group + head;
+              if (key < D) a.out[tok * a.ots + h * a.ohs + key] = __float2bfloat16_rn(l[r] == 0.f ? 0.f : o[r] / l[r]);
+              if (a.lse && key == 0)
+                a.lse[static_cast<int64_t>(tok) * a.Hq + h] = l[r] == 0.f ? -INFINITY : (ref[r] - kShift + log2f(l[r])) * 0.69314718055994531f;
+            } else {
+              if (key < D) part[r * D + key] = o[r];
+              if (key == 0) {
+                part[R * D + r] = ref[r];
+                part[R * D + R + r] = l[r];
+              }
+            }
+          }
+          if (++head == a.group) {
+            head = 0;
+            ++tok;
+          }
+        }
+        if (!whole) shared[n_shared++ & 1] = walk.g;  // (two at most: the run's first and its last)
+      }
+      group_sync(group);  // (red is free again)
+    }
+    // ---- items that other CTAs have parts of: the last one to get here joins them
+    for (int i = 0; i < n_shared; ++i) {
+      const Kv8Segment g = shared[i];
+      group_sync(group);
+      if (key == 0) {
+        bool last = false;
+        if (ok) {  // (what the group has written before the barrier goes before, what it reads behind it comes after)
+          int32_t ticket;
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(w.tickets + g.first_cta) : "memory");
+          last = ticket == g.last_cta - g.first_cta;
+        }
+        if (last) w.tickets[g.first_cta] = 0;
+        sm.red[group][0][0] = last ? 1.f : 0.f;
+      }
+      group_sync(group);
+      const bool last = sm.red[group][0][0] != 0.f;
+      if (last) join_parts<D, R>(a, w, g, key);
+      group_sync(group);
     }
   }
   tc_fence_before();
@@ -555,12 +655,13 @@ cudaError_t launch_one(const Kv8AttendArgs& a, Kv8Work w, int64_t rows, int ctas
   w.tile_rows = R;
   w.tiles = static_cast<int>((rows + R - 1) / R);
   w.items = static_cast<int64_t>(a.rows.batch) * a.Hkv * w.tiles;
-  w.step_pages = DecodeShape<D, R>::kPages;
-  w.min_steps = 4;
+  w.step_pages = 2;
+  w.min_steps = 16;
+  w.item_steps = 4;
   w.slot_floats = static_cast<int64_t>(kv8_decode_slot(D));
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(DecodeShape<D, R>::kThreads);
   cfg.dynamicSmemBytes = smem_bytes<D, R>();
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
@@ -573,7 +674,9 @@ cudaError_t launch_one(const Kv8AttendArgs& a, Kv8Work w, int64_t rows, int ctas
 template <int D>
 cudaError_t launch_dim(const Kv8AttendArgs& a, const Kv8Work& w, int ctas, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
   const int64_t rows = static_cast<int64_t>(a.rows.max_rows) * a.group;
-  return rows <= 8    ? launch_one<D, 8>(a, w, rows, ctas, tm_k, tm_v, st)
+  return rows <= 2    ? launch_one<D, 2>(a, w, rows, ctas, tm_k, tm_v, st)
+         : rows <= 4  ? launch_one<D, 4>(a, w, rows, ctas, tm_k, tm_v, st)
+         : rows <= 8  ? launch_one<D, 8>(a, w, rows, ctas, tm_k, tm_v, st)
          : rows <= 16 ? launch_one<D, 16>(a, w, rows, ctas, tm_k, tm_v, st)
                       : launch_one<D, 32>(a, w, rows, ctas, tm_k, tm_v, st);
 }
@@ -584,7 +687,9 @@ int kv8_decode_rows(int) { return 32; }
 size_t kv8_decode_slot(int D) { return static_cast<size_t>(32) * (D + 2); }
 
 cudaError_t kv8_decode_init(int D) {
-  cudaError_t e = D == 128 ? init_one<128, 8>() : init_one<64, 8>();
+  cudaError_t e = D == 128 ? init_one<128, 2>() : init_one<64, 2>();
+  if (e == cudaSuccess) e = D == 128 ? init_one<128, 4>() : init_one<64, 4>();
+  if (e == cudaSuccess) e = D == 128 ? init_one<128, 8>() : init_one<64, 8>();
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 16>() : init_one<64, 16>();
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 32>() : init_one<64, 32>();
   return e;
