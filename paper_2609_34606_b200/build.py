@@ -10,7 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libhsa.so")
 SOURCES = ["hsa_api.cu", "append.cu", "select.cu", "forward.cu", "linear_causal.cu", "linformer.cu", "linear_only.cu", "retrieve.cu",
-           "rope.cu", "kv8_api.cu", "kv8_append.cu", "kv8_attend.cu", "kv8_decode.cu"]
+           "rope.cu", "kv8_api.cu", "kv8_append.cu", "kv8_decode.cu", "kv8_chunk.cu"]
 
 
 def nvcc_path() -> str:

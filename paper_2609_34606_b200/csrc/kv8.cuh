@@ -87,12 +87,13 @@ struct Kv8Work {
   int tile_rows;       // query rows of an item
   int tiles;           // tiles of a sequence with max_rows rows
   int step_pages;
+  int half_rows;       // items of at most so many rows take twice the pages in a step
   int min_steps;       // an item is not cut into shorter parts while there is a CTA for each part
   int item_steps;      // steps that an item costs beside its own: runs are cut as if they came before them
   int64_t items;       // batch * Hkv * tiles
   float* parts;        // [2 * CTAs][slot_floats]
   int64_t slot_floats;
-  int32_t* tickets;    // [CTAs], zero between calls
+  int32_t* tickets;    // [2 * CTAs], zero between calls
 };
 
 int kv8_decode_rows(int D);                                   // rows up to which the kernel for few rows takes a call
@@ -100,7 +101,10 @@ size_t kv8_decode_slot(int D);                                // floats of a par
 cudaError_t kv8_decode_init(int D);
 cudaError_t launch_kv8_decode(const Kv8AttendArgs& a, Kv8Work w, int D, int nsm, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                               cudaStream_t st);
-cudaError_t launch_kv8_attend_plain(const Kv8AttendArgs& a, int D, cudaStream_t st);
+size_t kv8_chunk_slot(int D);
+cudaError_t kv8_chunk_init(int D);
+cudaError_t launch_kv8_chunk(const Kv8AttendArgs& a, Kv8Work w, int D, int nsm, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                             cudaStream_t st);
 
 __device__ __forceinline__ void kv8_flag(int32_t* status, int code) { atomicCAS(status, 0, code); }
 
@@ -142,7 +146,8 @@ __device__ __forceinline__ Kv8Item kv8_item(const Kv8AttendArgs& a, const Kv8Wor
   } else {
     it.pages = (it.limit(a, it.rows - 1) + kBlock - 1) / kBlock;
   }
-  it.steps = max(1, (it.pages + w.step_pages - 1) / w.step_pages);
+  const int pages = it.rows <= w.half_rows ? 2 * w.step_pages : w.step_pages;
+  it.steps = max(1, (it.pages + pages - 1) / pages);
   return it;
 }
 
@@ -182,7 +187,6 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
   constexpr int W = THREADS / 32;
   __shared__ int64_t sums[W];
   __shared__ int counts[W];
-  __shared__ int before_first;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
   const bool one = w.items <= THREADS;  // every thread has one item at most: once is enough
   int64_t total = 0;

@@ -63,10 +63,14 @@ bool on_device(hsa_kv8* ctx) {
 
 // workspace: status word, tickets, parts
 constexpr int kMaxCtas = 160;  // CTAs of an attention launch (one to an SM)
-constexpr size_t kStatusBytes = 256, kTicketBytes = 1024;
-static_assert(kMaxCtas * 4 <= kTicketBytes, "a ticket to a CTA");
+constexpr size_t kStatusBytes = 256, kTicketBytes = 1280;
+static_assert(2 * kMaxCtas * 4 <= kTicketBytes, "two tickets to a CTA");
 
-size_t part_floats(const hsa_kv8_config* c) { return kv8_decode_slot(c->head_dim); }
+// floats of a part: what the kernel for many rows leaves, where a call can have that many
+size_t part_floats(const hsa_kv8_config* c) {
+  const int64_t rows = static_cast<int64_t>(c->max_tokens) * (c->num_heads / c->num_kv_heads);
+  return rows > kv8_decode_rows(c->head_dim) ? kv8_chunk_slot(c->head_dim) : kv8_decode_slot(c->head_dim);
+}
 
 // A pool as rows of head_dim bytes, read a page tile (64 rows) at a time into the swizzle that spans a row.
 bool encode_pool(CUtensorMap* tm, void* base, uint64_t rows, int D) {
@@ -124,6 +128,7 @@ int hsa_kv8_create(hsa_kv8** out, const hsa_kv8_config* cfg, const hsa_kv8_buffe
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = kv8_append_init(cfg->head_dim);
   if (e == cudaSuccess) e = kv8_decode_init(cfg->head_dim);
+  if (e == cudaSuccess) e = kv8_chunk_init(cfg->head_dim);
   const uint64_t rows = static_cast<uint64_t>(cfg->max_pages) * cfg->num_kv_heads * kBlock;
   if (e != cudaSuccess || !encode_pool(&ctx->tm_k, b->k_pool, rows, cfg->head_dim) ||
       !encode_pool(&ctx->tm_v, b->v_pool, rows, cfg->head_dim)) {
@@ -212,7 +217,7 @@ int hsa_kv8_attend(hsa_kv8* ctx, const void* q, int32_t n_tokens, int32_t batch,
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = static_cast<int64_t>(max_q) * a.group <= kv8_decode_rows(c.head_dim)
                             ? launch_kv8_decode(a, w, c.head_dim, ctas, ctx->tm_k, ctx->tm_v, st)
-                            : launch_kv8_attend_plain(a, c.head_dim, st);
+                            : launch_kv8_chunk(a, w, c.head_dim, ctas, ctx->tm_k, ctx->tm_v, st);
   return e == cudaSuccess ? HSA_OK : cuda_fail(ctx, e);
 }
 

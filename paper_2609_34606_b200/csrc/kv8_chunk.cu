@@ -1,0 +1,726 @@
+// Attention over the 8-bit paged cache for many query rows of a key head: chunks, prompts.
+//
+// Here the operations bound the call, 4 * D for every pair of a query and a key, and what the tensor cores do not do has to
+// fit beside them: an exponential for every pair (16 a clock on an SM, which is what the products of D = 128 take as well)
+// and the values' way from 8 bits to 16.
+//   S [128 rows x 128 keys] = (Qhi + Qlo) [128 x D] K^T [D x 128]    e4m3 codes as TMA leaves them; the queries in two terms,
+//                                                                    which together take as long as one product of bf16
+//   O [128 rows x D]       += P [128 x 128 keys] V [128 x D]         bf16: P from tensor memory, V from shared memory
+// A query is hi = e4m3(x), lo = e4m3(x - hi), x scaled by a power of two that brings its row's largest value to 2^7 .. 2^8:
+// bf16 values stay exact unless they are below 2^-10 of that, which may lose 2^-18 of it.  The keys' scales are left to the
+// softmax, where they are part of the factor that scores are multiplied by anyhow.  The values become bf16 with their scale in
+// them, which is exact: a code has 4 significant bits, and bf16 has the range of fp32.  So weights need no more than bf16
+// either, whatever the scales of other pages are.
+//
+// An item has 256 rows, two tiles of 128 that take turns on the tensor cores: while one tile's scores go through the
+// exponentials, the other's products run, and every page that is read and turned into bf16 serves both.  An item of 128 rows or
+// fewer gives both tiles to the same rows: they take the steps of 128 keys in turn and are brought together at its end.
+//
+// Warps: 0 loads pages, 1 issues the products, 4 - 7 turn values into bf16 and, an item ahead, queries into their two terms, 8 - 11
+// and 12 - 15 are the softmax of a tile each, a row to a thread.
+// Tensor memory: S of both tiles (P, packed bf16, over its first half), O of both tiles.
+#include "kv8.cuh"
+#include "kv8_mma.cuh"
+
+namespace hsa {
+
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kTile = 128;          // rows of a tile; keys of a step
+constexpr float kGrow = 8.f;        // a row's reference is set anew when a score passes it by 2^8: sums and O have room for that
+constexpr int kMetas = 8;
+
+template <int D>
+struct ChunkSmem {
+  static constexpr int kPage = kBlock * D;
+  static constexpr int kStage = 2 * kPage;
+  static constexpr int kKStages = D == 128 ? 3 : 6, kVStages = D == 128 ? 2 : 4;
+  union {
+    uint8_t q[2][2][kTile * D];        // [tile][term]
+    float other[D][kTile];             // O of the second tile, where both have the same rows
+  };
+  uint8_t k[kKStages][kStage];
+  uint8_t vc[kVStages][kStage];        // codes
+  uint8_t vb[2][kTile * D * 2];        // bf16, [64 dims][key][64 dims], dims of a group of four in the order 0, 2, 1, 3
+  float qscale[2 * kTile];
+  float other_ref[kTile], other_sum[kTile];
+  PageMeta meta[kMetas][2];
+  int last[2];
+  uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[2], vb_empty[2];
+  uint64_t s_full[2], p_full[2][2], o_done[2], q_full, q_free, other_full, done;
+  uint32_t tmem;
+  Kv8Plan plan;
+};
+
+constexpr uint32_t kColS = 0, kColO = 256;  // + 128 a tile
+
+// ---- two fp32 in a register pair
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float2 unpair(uint64_t d) {
+  float2 f;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(d));
+  return f;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float m;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+  return m;
+}
+
+// 2^x of a pair without the special function unit: x = n + f, |f| <= 1/2, by adding and taking away 1.5 * 2^23; 2^f as the
+// polynomial of degree 4 with p(0) = 1 whose relative error, 2.9e-6, is least on that interval (found by linear programming);
+// n goes into the exponent.  Values below 2^-126 come out as that.
+__device__ __forceinline__ uint64_t ex2_poly(uint64_t x) {
+  float2 v = unpair(x);
+  const uint64_t y = pair(fmaxf(v.x, -126.f), fmaxf(v.y, -126.f));
+  const uint64_t magic = pair(12582912.f, 12582912.f), minus = pair(-12582912.f, -12582912.f);
+  const uint64_t t = add2(y, magic);
+  const uint64_t f = fma2(add2(t, minus), pair(-1.f, -1.f), y);
+  uint64_t p = pair(0.009582576647f, 0.009582576647f);
+  p = fma2(p, f, pair(0.05590682995f, 0.05590682995f));
+  p = fma2(p, f, pair(0.2402410727f, 0.2402410727f));
+  p = fma2(p, f, pair(0.6931241184f, 0.6931241184f));
+  p = fma2(p, f, pair(1.f, 1.f));
+  const float2 pf = unpair(p), tf = unpair(t);
+  return pair(__uint_as_float(__float_as_uint(pf.x) + (__float_as_uint(tf.x) << 23)),
+              __uint_as_float(__float_as_uint(pf.y) + (__float_as_uint(tf.y) << 23)));
+}
+
+// Weights of 32 keys: 2^(s * c - ref) as bf16 pairs, and their sums in fp32.  POLY of every 16 are polynomials.
+template <int POLY>
+__device__ __forceinline__ void weights(const uint32_t* s, float c, float nref, uint64_t* sum, uint32_t* w) {
+  const uint64_t c2 = pair(c, c), r2 = pair(nref, nref);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    uint64_t y = fma2(pair(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, r2);
+    if ((i * POLY) % 16 < POLY) {
+      y = ex2_poly(y);
+    } else {
+      const float2 f = unpair(y);
+      y = pair(ex2(f.x), ex2(f.y));
+    }
+    sum[i & 1] = add2(sum[i & 1], y);
+    const float2 f = unpair(y);
+    w[i] = pack_bf16(f.x, f.y);
+  }
+}
+
+// Four e4m3 codes as bf16: (0, 2) and (1, 3).  A code's bits, put where bf16 has them, are the value times 2^-120, subnormal
+// ones too, and there is no code that gives Inf or NaN; the rest is a product by a power of two, or by two of them (m1, m2) where one would pass the range.
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ void codes_to_bf16(uint32_t w, uint32_t m1, uint32_t* even, uint32_t* odd) {
+  *even = mul_bf16x2(((w << 8) & 0x80008000u) | ((w << 4) & 0x07f007f0u), m1);
+  *odd = mul_bf16x2((w & 0x80008000u) | ((w >> 4) & 0x07f007f0u), m1);
+}
+
+__device__ __forceinline__ uint32_t e4m3x2(float a, float b) { return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3); }
+__device__ __forceinline__ float2 from_e4m3x2(uint32_t two) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// D dims of the output's row: columns of four come as 0, 2, 1, 3.
+__device__ __forceinline__ void to_order(uint32_t* o) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    const uint32_t t = o[i + 1];
+    o[i + 1] = o[i + 2];
+    o[i + 2] = t;
+  }
+}
+
+__device__ __forceinline__ void tile_sync(int tile) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + tile) : "memory"); }
+
+// A part: a tile's O (fp32, unnormalised) as [D / 4][row][4], the rows' references and sums.
+template <int D>
+__device__ __forceinline__ float* part_of(const Kv8Work& w, int64_t slot, int tile) {
+  return w.parts + slot * w.slot_floats + tile * (kTile * (D + 2));
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+  using Smem = ChunkSmem<D>;
+  constexpr int kKStages = Smem::kKStages, kVStages = Smem::kVStages, kPage = Smem::kPage, kStage = Smem::kStage;
+  extern __shared__ uint8_t smem_raw[];
+  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+  if (tid == 0) {
+    for (int i = 0; i < kKStages; ++i) {
+      mbar_init(&sm.k_full[i], 1);
+      mbar_init(&sm.k_empty[i], 1);
+    }
+    for (int i = 0; i < kVStages; ++i) {
+      mbar_init(&sm.vc_full[i], 1);
+      mbar_init(&sm.vc_empty[i], 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sm.vb_full[i], 4);
+      mbar_init(&sm.vb_empty[i], 1);
+      mbar_init(&sm.s_full[i], 1);
+      mbar_init(&sm.p_full[i][0], 4);
+      mbar_init(&sm.p_full[i][1], 4);
+      mbar_init(&sm.o_done[i], 1);
+    }
+    mbar_init(&sm.q_full, 4);
+    mbar_init(&sm.q_free, 1 + 8);  // its products, and the softmax warps (scales; the merge of two tiles)
+    mbar_init(&sm.other_full, 4);
+    mbar_init(&sm.done, 1);
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  if (warp == 1) {
+    tmem_alloc(&sm.tmem, 512);
+    tmem_relinquish();
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  kv8_plan<kThreads>(a, w, &sm.plan);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+  Kv8Walk walk;
+  bool ok = true;  // false: a wait ran out; nothing more is waited for
+  const auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (ok && !mbar_wait(bar, parity)) {
+      ok = false;
+      kv8_flag(a.status, kDevTimeout);
+    }
+    return ok;
+  };
+  // the same for a whole warp that stays together
+  const auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
+  // both tiles of the item on the same rows?
+  const auto shared_rows = [](const Kv8Item& it) { return it.rows <= kTile; };
+
+  // The CTA is allocated 128 registers a thread.  Half of them give back 48, which the softmax warps take.
+  static_assert(256 * (128 - 80) >= 256 * (176 - 128), "setmaxnreg.inc would never be satisfied");
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 0) {
+      // ---- loads.  The lanes look up the pages of 16 steps at once.
+      uint32_t n = 0;
+      while (ok && walk.next(a, w, sm.plan)) {
+        const Kv8Item& it = walk.g.it;
+        const int per = shared_rows(it) ? 2 : 1, s1 = walk.g.s1 * per;  // steps of 128 keys
+        for (int s = walk.g.s0 * per; s < s1 && ok; s += 16) {
+          int blk = 0, page = -1;
+          PageMeta meta{-1, 1.f, 0.f};
+          if (s + lane / 2 < s1) page = kv8_page(a, it, s * 2 + lane, &blk);
+          if (page >= 0) {
+            const int64_t ph = static_cast<int64_t>(page) * a.Hkv + it.h;
+            meta.pos = blk * kBlock;
+            meta.ks = __ldg(a.k_scale + ph);
+            meta.vs = __ldg(a.v_scale + ph);
+          }
+          const int count = min(16, s1 - s);
+          for (int i = 0; i < count; ++i, ++n) {
+            const uint32_t st = n % kKStages, sv = n % kVStages;
+            if (!warp_wait(&sm.k_empty[st], ((n / kKStages) & 1) ^ 1)) break;
+            int pages[2], bytes = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              pages[j] = __shfl_sync(0xffffffffu, page, i * 2 + j);
+              if (pages[j] >= 0) bytes += kPage;
+            }
+            // the loads go out before the scales are there; the barrier is arrived at behind them
+            if (elect_one_sync()) {
+              if (bytes) mbar_expect_tx_only(&sm.k_full[st], bytes);
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                if (pages[j] >= 0)
+                  tma_load_2d(sm.k[st] + j * kPage, &tm_k, &sm.k_full[st], 0,
+                              static_cast<int>((static_cast<int64_t>(pages[j]) * a.Hkv + it.h) * kBlock));
+            }
+            if (lane / 2 == i) sm.meta[n % kMetas][lane % 2] = meta;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.k_full[st]);
+            if (!warp_wait(&sm.vc_empty[sv], ((n / kVStages) & 1) ^ 1)) {
+              if (lane == 0) mbar_arrive(&sm.vc_full[sv]);
+              ++n;
+              break;
+            }
+            if (elect_one_sync()) {
+              if (bytes) mbar_expect_tx(&sm.vc_full[sv], bytes);
+              else mbar_arrive(&sm.vc_full[sv]);
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                if (pages[j] >= 0)
+                  tma_load_2d(sm.vc[sv] + j * kPage, &tm_v, &sm.vc_full[sv], 0,
+                              static_cast<int>((static_cast<int64_t>(pages[j]) * a.Hkv + it.h) * kBlock));
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!ok) {  // pages that nobody took: their loads must not outlive the CTA
+        for (uint32_t i = 1; i <= kKStages && i <= n; ++i) mbar_wait(&sm.k_full[(n - i) % kKStages], ((n - i) / kKStages) & 1);
+        for (uint32_t i = 1; i <= kVStages && i <= n; ++i) mbar_wait(&sm.vc_full[(n - i) % kVStages], ((n - i) / kVStages) & 1);
+      }
+    } else if (warp == 1) {
+      // ---- products
+      if (elect_one_sync()) {
+        constexpr uint32_t id_s = idesc_e4m3(128, 128, 0, 0), id_o = idesc_bf16_f32(128, D, 0, 1), hi_v = desc_hi_sw128(1024);
+        const uint64_t q0 = row_desc<D>(smem_u32(sm.q), 0), k0 = row_desc<D>(smem_u32(sm.k), 0);
+        const uint32_t v0 = desc_lo_sw128(smem_u32(sm.vb), kTile * 128);
+        uint32_t items = 0, nk = 0, nv = 0, np[2] = {0, 0};  // items; steps whose keys, values have been seen; weights of a tile
+        while (ok && walk.next(a, w, sm.plan)) {
+          const bool same = shared_rows(walk.g.it);
+          const int units = 2 * (walk.g.s1 - walk.g.s0);  // unit u: tile u % 2 at its next step
+          if (!wait(&sm.q_full, items & 1)) break;
+          const auto scores = [&](int u) {
+            const int t = u & 1;
+            const uint32_t st = nk % kKStages;
+            if (same || t == 0) {
+              if (!wait(&sm.k_full[st], (nk / kKStages) & 1)) return;
+              tc_fence_after();
+            }
+            const uint64_t q = q0 + ((same ? 0 : t) * 2 * kTile * D) / 16, k = k0 + (st * kStage) / 16;
+#pragma unroll
+            for (int term = 0; term < 2; ++term)
+#pragma unroll
+              for (int kk = 0; kk < D / 32; ++kk)
+                mma_f8(tmem + kColS + t * 128, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, id_s, term + kk > 0);
+            tc_commit(&sm.s_full[t]);
+            if (same || t == 1) {
+              tc_commit(&sm.k_empty[st]);
+              ++nk;
+            }
+            if (u == units - 1) tc_commit(&sm.q_free);
+          };
+          scores(0);
+          scores(1);
+          for (int u = 0; u < units && ok; ++u) {
+            const int t = u & 1;
+            const uint32_t b = nv & 1;
+            const uint32_t v = v0 + (b * (kTile * D * 2)) / 16;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              if (!wait(&sm.p_full[t][half], np[t] & 1)) break;
+              if (half == 0 && (same || t == 0) && !wait(&sm.vb_full[b], (nv / 2) & 1)) break;
+              tc_fence_after();
+#pragma unroll
+              for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+                tc_mma_ts_lo(tmem + kColO + t * 128, tmem + kColS + t * 128 + kk * 8, v + kk * 128, hi_v, id_o, u >= 2 || kk > 0);
+            }
+            ++np[t];
+            if (same || t == 1) {
+              tc_commit(&sm.vb_empty[b]);
+              ++nv;
+            }
+            if (u >= units - 2) tc_commit(&sm.o_done[t]);
+            if (u + 2 < units && ok) scores(u + 2);
+          }
+          ++items;
+        }
+        tc_commit(&sm.done);
+        mbar_wait(&sm.done, 0);
+      }
+      __syncwarp();
+    }
+  } else if (warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    // ---- queries into two terms, values into bf16
+    const int c = tid - 128;
+    uint32_t items = 0, n = 0;
+    while (walk.next(a, w, sm.plan)) {
+      const Kv8Item& it = walk.g.it;
+      {
+        constexpr int V = D / 8, R = 128 / V, kAtOnce = 4;  // vectors of a row, rows at a time, of which so many are in flight
+        const int r0 = c / V, e = c % V;
+        const int rows = shared_rows(it) ? kTile : 2 * kTile;
+        bool waited = false;
+        for (int base = 0; base < rows; base += R * kAtOnce) {
+          uint4 in[kAtOnce];
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) {
+            const int r = base + i * R + r0;
+            in[i] = make_uint4(0, 0, 0, 0);
+            if (r < it.rows) {
+              const int at = it.row0 + r;
+              in[i] = __ldg(reinterpret_cast<const uint4*>(a.q + (it.first + at / a.group) * a.ts + (it.h * a.group + at % a.group) * a.hs + e * 8));
+            }
+          }
+          if (!waited) {
+            warp_wait(&sm.q_free, (items & 1) ^ 1);
+            waited = true;
+          }
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) {
+            const int r = base + i * R + r0;
+            const uint32_t words[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
+            float x[8];
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              x[j] = __uint_as_float(j & 1 ? words[j / 2] & 0xffff0000u : words[j / 2] << 16);
+              // (what is not finite: NaN, which spoils the row and no other)
+              if (fabsf(x[j]) < INFINITY) top = fmaxf(top, fabsf(x[j]));
+              else x[j] = NAN;
+            }
+#pragma unroll
+            for (int o = V / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const int ex = max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100) - 7;  // (rows of zeros: any will do)
+            const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float y0 = x[2 * j] * up, y1 = x[2 * j + 1] * up;
+              hi[j] = e4m3x2(y0, y1);
+              const float2 h = from_e4m3x2(hi[j]);
+              lo[j] = e4m3x2(y0 - h.x, y1 - h.y);
+            }
+            uint8_t* q = sm.q[r / kTile][0] + swizzled<D>(r % kTile, e * 8);
+            *reinterpret_cast<uint2*>(q) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+            *reinterpret_cast<uint2*>(q + kTile * D) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+            if (e == 0) sm.qscale[r] = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23) * a.scale_log2;
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.q_full);
+        ++items;
+      }
+      const int steps = (walk.g.s1 - walk.g.s0) * (shared_rows(it) ? 2 : 1);
+      constexpr int C = D / 16, R = 128 / C;  // 16 dims of a row, rows at a time
+      const int r0 = c / C, e = c % C;
+      for (int s = 0; s < steps; ++s, ++n) {
+        const uint32_t sv = n % kVStages, b = n & 1;
+        warp_wait(&sm.vc_full[sv], (n / kVStages) & 1);
+        warp_wait(&sm.vb_empty[b], ((n / 2) & 1) ^ 1);
+        uint8_t* to = sm.vb[b] + (e / 4) * (kTile * 128);
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+          const float vs = sm.meta[n % kMetas][pg].vs;
+          // 2^120 vs, in one factor where it fits
+          const bool two = vs > 64.f;
+          const float f1 = two ? 0x1p120f : vs * 0x1p60f * 0x1p60f;
+          const uint32_t m1 = pack_bf16(f1, f1), m2 = pack_bf16(vs, vs);
+          const uint8_t* from = sm.vc[sv] + pg * kPage;
+          uint4 in[kBlock / R];
+#pragma unroll
+          for (int i = 0; i < kBlock / R; ++i) in[i] = *reinterpret_cast<const uint4*>(from + swizzled<D>(i * R + r0, e * 16));
+#pragma unroll
+          for (int i = 0; i < kBlock / R; ++i) {
+            const int row = pg * kBlock + i * R + r0;
+            uint4 out[2];
+            codes_to_bf16(in[i].x, m1, &out[0].x, &out[0].y);
+            codes_to_bf16(in[i].y, m1, &out[0].z, &out[0].w);
+            codes_to_bf16(in[i].z, m1, &out[1].x, &out[1].y);
+            codes_to_bf16(in[i].w, m1, &out[1].z, &out[1].w);
+            if (two) {
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                out[j] = make_uint4(mul_bf16x2(out[j].x, m2), mul_bf16x2(out[j].y, m2), mul_bf16x2(out[j].z, m2), mul_bf16x2(out[j].w, m2));
+            }
+            // (lanes of the upper slab store their second half first: no two of eight lanes meet in a bank)
+            const bool flip = (e & 4) != 0;
+            const int c0 = (e & 3) * 2;
+            *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 1 : 0)) ^ (row & 7)) << 4)) = flip ? out[1] : out[0];
+            *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 0 : 1)) ^ (row & 7)) << 4)) = flip ? out[0] : out[1];
+          }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&sm.vb_full[b]);
+          mbar_arrive(&sm.vc_empty[sv]);
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    // ---- softmax: a thread is a row of the tile.  After a wait that ran out the threads go on with whatever is there,
+    // because they meet at barriers; the status word says that the result is none.
+    const int t = (warp - 8) / 4, r = (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
+    uint32_t items = 0, n = 0, kn = 0, merges = 0;  // items, units of this tile, steps of 128 keys before the item's first
+    Kv8Segment cut0, cut1;  // of the items that the run shares with others: its first and its last
+    int n_cut = 0;
+    while (walk.next(a, w, sm.plan)) {
+      const Kv8Item& it = walk.g.it;
+      const bool same = shared_rows(it);
+      const int units = walk.g.s1 - walk.g.s0;
+      const int row = same ? r : t * kTile + r;  // of the item
+      const int lim = it.limit(a, min(row, it.rows - 1)), lim_low = it.limit(a, same ? 0 : t * kTile);
+      wait(&sm.q_full, items & 1);
+      __syncwarp();
+      const float qs = sm.qscale[row];
+      if (!same) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.q_free);
+      }
+      float ref = kNone;
+      uint64_t sum[2] = {0, 0};
+      for (int u = 0; u < units; ++u, ++n) {
+        const PageMeta* meta = sm.meta[(kn + (same ? 2 * u + t : u)) % kMetas];
+        wait(&sm.s_full[t], n & 1);
+        __syncwarp();
+        tc_fence_after();
+        uint32_t x[128];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld32(col_s + i * 32, *reinterpret_cast<uint32_t(*)[32]>(x + i * 32));
+        const int pos0 = meta[0].pos, pos1 = meta[1].pos;
+        const float c0 = fmaxf(qs * meta[0].ks, 0x1p-126f), c1 = fmaxf(qs * meta[1].ks, 0x1p-126f);  // (never 0: scores may be -inf)
+        const bool masked = min(pos0, pos1) < 0 || max(pos0, pos1) + kBlock > lim_low;
+        tc_wait_ld();
+        if (masked) {
+          const int lim0 = pos0 < 0 ? 0 : lim - pos0, lim1 = pos1 < 0 ? 0 : lim - pos1;
+#pragma unroll
+          for (int i = 0; i < 64; ++i) {
+            if (i >= lim0) x[i] = 0xff800000u;
+            if (i >= lim1) x[64 + i] = 0xff800000u;
+          }
+        }
+        float top;
+        {
+          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 64; i += 4) {
+            m[0] = max3(m[0], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+            m[1] = max3(m[1], __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+            m[2] = max3(m[2], __uint_as_float(x[64 + i]), __uint_as_float(x[64 + i + 1]));
+            m[3] = max3(m[3], __uint_as_float(x[64 + i + 2]), __uint_as_float(x[64 + i + 3]));
+          }
+          top = fmaxf(fmaxf(m[0], m[1]) * c0, fmaxf(m[2], m[3]) * c1);
+        }
+        if (__any_sync(0xffffffffu, top > ref + kGrow)) {
+          const float to = top > ref + kGrow ? top : ref, f = ex2(ref - to);
+          ref = to;
+          const uint64_t f2 = pair(f, f);
+          sum[0] = fma2(sum[0], f2, 0);
+          sum[1] = fma2(sum[1], f2, 0);
+          // (the scores came behind the products before them: O is at rest)
+          if (u > 0) {
+#pragma unroll 1
+            for (int i = 0; i < D; i += 16) {
+              uint32_t o[16];
+              tmem_ld16(col_o + i, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st16(col_o + i, o);
+            }
+          }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const float c = half ? c1 : c0;
+          uint32_t p[32];
+          if (masked) {
+            weights<0>(x + half * 64, c, -ref, sum, p);
+            weights<0>(x + half * 64 + 32, c, -ref, sum, p + 16);
+          } else {
+            weights<4>(x + half * 64, c, -ref, sum, p);
+            weights<4>(x + half * 64 + 32, c, -ref, sum, p + 16);
+          }
+          tmem_st32(col_s + half * 32, p);
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.p_full[t][half]);
+        }
+      }
+      kn += units * (same ? 2 : 1);
+      const float2 s0 = unpair(sum[0]), s1 = unpair(sum[1]);
+      float l = (s0.x + s0.y) + (s1.x + s1.y);
+      wait(&sm.o_done[t], items & 1);
+      __syncwarp();
+      tc_fence_after();
+      ++items;
+      float down = 1.f, take = 0.f;  // what this tile's O counts, and the other's
+      if (same) {
+        if (t == 1) {
+#pragma unroll 1
+          for (int i = 0; i < D; i += 32) {
+            uint32_t o[32];
+            tmem_ld32(col_o + i, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sm.other[i + j][r] = __uint_as_float(o[j]);
+          }
+          sm.other_ref[r] = ref;
+          sm.other_sum[r] = l;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.other_full);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sm.q_free);
+          continue;
+        }
+        wait(&sm.other_full, merges & 1);
+        __syncwarp();
+        ++merges;
+        const float m = sm.other_ref[r], to = fmaxf(ref, m);
+        down = ex2(ref - to);
+        take = ex2(m - to);
+        l = fmaf(sm.other_sum[r], take, l * down);
+        ref = to;
+      }
+      const bool whole = walk.g.whole();
+      const bool real = row < it.rows && ok;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int at = it.row0 + min(row, it.rows - 1), head = it.h * a.group + at % a.group;
+      const int64_t tok = it.first + at / a.group;
+      float* part = part_of<D>(w, walk.g.slot(), t);
+#pragma unroll 1
+      for (int i = 0; i < D; i += 32) {
+        uint32_t o[32];
+        tmem_ld32(col_o + i, o);
+        tc_wait_ld();
+        if (same) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(sm.other[i + j][r], take, __uint_as_float(o[j]) * down));
+        }
+        to_order(o);
+        if (real && whole) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) {
+            uint32_t y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              y[k] = pack_bf16(__uint_as_float(o[j + 2 * k]) * inv, __uint_as_float(o[j + 2 * k + 1]) * inv);
+            *reinterpret_cast<uint4*>(a.out + tok * a.ots + head * a.ohs + i + j) = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        }
+        if (real && !whole) {
+#pragma unroll
+          for (int j = 0; j < 32; j += 4)
+            __stcg(reinterpret_cast<uint4*>(part) + ((i + j) / 4) * kTile + r, make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+        }
+        __syncwarp();
+      }
+      if (real) {
+        if (whole) {
+          if (a.lse) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
+        } else {
+          __stcg(part + kTile * D + r, ref);
+          __stcg(part + kTile * D + kTile + r, l);
+        }
+      }
+      __syncwarp();
+      if (same && lane == 0) mbar_arrive(&sm.q_free);
+      if (!whole) {
+        if (n_cut++ == 0) cut0 = walk.g;
+        else cut1 = walk.g;
+      }
+    }
+    // ---- items that other CTAs have parts of: the last one to get here joins them
+    for (int i = 0; i < n_cut; ++i) {
+      const Kv8Segment g = i == 0 ? cut0 : cut1;
+      tile_sync(t);
+      if (r == 0) {
+        bool last = false;
+        if (ok) {  // (what the tile has written before the barrier goes before, what it reads behind it comes after)
+          int32_t* at = w.tickets + 2 * g.first_cta + t;
+          int32_t ticket;
+          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(at) : "memory");
+          last = ticket == g.last_cta - g.first_cta;
+          if (last) *at = 0;
+        }
+        sm.last[t] = last;
+      }
+      tile_sync(t);
+      const int row = shared_rows(g.it) ? r : t * kTile + r;
+      if (sm.last[t] && row < g.it.rows) {
+        float m = kNone;
+        for (int j = g.first_cta; j <= g.last_cta; ++j)
+          m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
+        const int at = g.it.row0 + row, head = g.it.h * a.group + at % a.group;
+        const int64_t tok = g.it.first + at / a.group;
+        float l = 0.f;
+        for (int half = 0; half < 2; ++half) {
+          float4 o[D / 8];
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          l = 0.f;
+          for (int j = g.first_cta; j <= g.last_cta; ++j) {
+            const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t);
+            const float f = ex2(__ldcg(p + kTile * D + r) - m);
+            l = fmaf(__ldcg(p + kTile * D + kTile + r), f, l);
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k) {
+              const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + (half * (D / 8) + k) * kTile + r);
+              o[k].x = fmaf(v.x, f, o[k].x);
+              o[k].y = fmaf(v.y, f, o[k].y);
+              o[k].z = fmaf(v.z, f, o[k].z);
+              o[k].w = fmaf(v.w, f, o[k].w);
+            }
+          }
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+          for (int k = 0; k < D / 8; ++k)
+            *reinterpret_cast<uint2*>(a.out + tok * a.ots + head * a.ohs + half * (D / 2) + k * 4) =
+                make_uint2(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv));
+        }
+        if (a.lse) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+template <int D>
+constexpr size_t smem_bytes() {
+  static_assert(sizeof(ChunkSmem<D>) + 1024 <= 232448, "shared memory of an SM");
+  return sizeof(ChunkSmem<D>) + 1024;
+}
+
+}  // namespace
+
+size_t kv8_chunk_slot(int D) { return static_cast<size_t>(2 * kTile) * (D + 2); }
+
+cudaError_t kv8_chunk_init(int D) {
+  return D == 128 ? cudaFuncSetAttribute(kv8_chunk_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<128>()))
+                  : cudaFuncSetAttribute(kv8_chunk_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<64>()));
+}
+
+cudaError_t launch_kv8_chunk(const Kv8AttendArgs& a, Kv8Work w, int D, int ctas, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
+                             cudaStream_t st) {
+  const int64_t rows = static_cast<int64_t>(a.rows.max_rows) * a.group;
+  w.tile_rows = 2 * kTile;
+  w.tiles = static_cast<int>((rows + 2 * kTile - 1) / (2 * kTile));
+  w.items = static_cast<int64_t>(a.rows.batch) * a.Hkv * w.tiles;
+  w.step_pages = 2;
+  w.half_rows = kTile;
+  w.min_steps = 4;
+  w.item_steps = 2;
+  w.slot_floats = static_cast<int64_t>(kv8_chunk_slot(D));
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = D == 128 ? smem_bytes<128>() : smem_bytes<64>();
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, D == 128 ? kv8_chunk_kernel<128> : kv8_chunk_kernel<64>, a, w, tm_k, tm_v);
+}
+
+}  // namespace hsa

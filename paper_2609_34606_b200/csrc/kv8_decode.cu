@@ -21,11 +21,8 @@
 // looking at barriers and issuing, the loads of a step take 1400), 2 prepares the rows of Q of the next item, then one or two
 // groups of four for softmax and output.  Two groups take the steps in turn, each with sums and references of its own, which they bring
 // together at an item's end; the group that had the item's last step writes it, while the other goes on.
-#include <cuda_fp8.h>
-#include <cuda_fp16.h>
-
 #include "kv8.cuh"
-#include "ptx.cuh"
+#include "kv8_mma.cuh"
 
 namespace hsa {
 
@@ -33,12 +30,6 @@ namespace {
 
 constexpr float kShift = 7.f;   // the largest weight is 2^7 when the reference is set ...
 constexpr float kSlack = 1.75f; // ... and may grow to 2^8.75 < 448 before it is set anew
-constexpr float kNone = -1e30f; // reference of a row that has seen nothing
-
-struct PageMeta {
-  int pos;      // position of the page's first token; < 0: nothing to see
-  float ks, vs; // scales; vs 0: no page
-};
 
 // R: rows of an item.  A step is a tile of 128 keys, two pages.
 template <int D, int R>
@@ -72,15 +63,6 @@ struct DecodeSmem {
   Kv8Plan plan;
 };
 
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// the bytes alone: the arrival comes later
-__device__ __forceinline__ void mbar_expect_tx_only(uint64_t* bar, uint32_t bytes) {
-  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
 // The four warps of a group meet; `any`: whether x holds for one of them.
 __device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + group) : "memory"); }
 __device__ __forceinline__ bool group_any(int group, bool x) {
@@ -102,33 +84,6 @@ __device__ __forceinline__ float warp_max(float x) {
   float y;
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
   return y;
-}
-
-__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n"
-      "}\n" ::"r"(d_tmem),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// kind::f8f6f4, e4m3 operands (format 0), fp32 accumulator; bits as idesc_bf16_f32
-__host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N, uint32_t a_mn, uint32_t b_mn) {
-  return (1u << 4) | (a_mn << 15) | (b_mn << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
-}
-// Rows of D bytes in the swizzle that spans a row (128 bytes: layout 2, 64 bytes: layout 4); eight rows are 8 * D bytes.
-template <int D>
-__device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo) {
-  return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(lbo >> 4) << 16 |
-         static_cast<uint64_t>((8 * D) >> 4) << 32 | static_cast<uint64_t>(1) << 46 |
-         static_cast<uint64_t>(D == 128 ? 2 : 4) << 61;
-}
-// Byte of (row, byte in the row) in such a tile.
-template <int D>
-__device__ __forceinline__ int swizzled(int row, int byte) {
-  return row * D + ((byte >> 4) ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16 + (byte & 15);
 }
 
 constexpr float kLow = 1.f / 16.f;  // what the second term counts
@@ -656,6 +611,7 @@ cudaError_t launch_one(const Kv8AttendArgs& a, Kv8Work w, int64_t rows, int ctas
   w.tiles = static_cast<int>((rows + R - 1) / R);
   w.items = static_cast<int64_t>(a.rows.batch) * a.Hkv * w.tiles;
   w.step_pages = 2;
+  w.half_rows = 0;
   w.min_steps = 16;
   w.item_steps = 4;
   w.slot_floats = static_cast<int64_t>(kv8_decode_slot(D));

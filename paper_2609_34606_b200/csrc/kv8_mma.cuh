@@ -1,0 +1,54 @@
+// What the two attention kernels over the 8-bit cache share of the tensor cores: e4m3 products and their operands' layouts.
+#pragma once
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "kv8.cuh"
+#include "ptx.cuh"
+
+namespace hsa {
+
+constexpr float kNone = -1e30f; // reference of a row that has seen nothing
+
+struct PageMeta {
+  int pos;      // position of the page's first token; < 0: nothing to see
+  float ks, vs; // scales; vs 0: no page
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// the bytes alone: the arrival comes later
+__device__ __forceinline__ void mbar_expect_tx_only(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// kind::f8f6f4, e4m3 operands (format 0), fp32 accumulator; bits as idesc_bf16_f32
+__host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N, uint32_t a_mn, uint32_t b_mn) {
+  return (1u << 4) | (a_mn << 15) | (b_mn << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
+}
+// Rows of D bytes in the swizzle that spans a row (128 bytes: layout 2, 64 bytes: layout 4); eight rows are 8 * D bytes.
+template <int D>
+__device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo) {
+  return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(lbo >> 4) << 16 |
+         static_cast<uint64_t>((8 * D) >> 4) << 32 | static_cast<uint64_t>(1) << 46 |
+         static_cast<uint64_t>(D == 128 ? 2 : 4) << 61;
+}
+// Byte of (row, byte in the row) in such a tile.
+template <int D>
+__device__ __forceinline__ int swizzled(int row, int byte) {
+  return row * D + ((byte >> 4) ^ (D == 128 ? row & 7 : (row >> 1) & 3)) * 16 + (byte & 15);
+}
+
+}  // namespace hsa
