@@ -121,7 +121,8 @@ struct Kv8Item {
   }
 };
 
-__device__ __forceinline__ Kv8Item kv8_item(const Kv8AttendArgs& a, const Kv8Work& w, int64_t i) {
+// (not inlined: a handful of places call it, seldom, and the kernels' roles share the instruction caches of an SM)
+__device__ __noinline__ static Kv8Item kv8_item(const Kv8AttendArgs& a, const Kv8Work& w, int64_t i) {
   Kv8Item it;
   const uint32_t at = static_cast<uint32_t>(i);  // (launches with 2^31 items are refused)
   it.tile = static_cast<int>(at % static_cast<uint32_t>(w.tiles));
@@ -208,7 +209,7 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
     }
     __syncthreads();
     int before = 0, all = 0;
-#pragma unroll
+#pragma unroll 4
     for (int j = 0; j < W; ++j) {
       if (j < warp) before += counts[j];
       all += counts[j];
@@ -230,6 +231,7 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
   }
   if (!one) {
     int64_t mine = 0;
+#pragma unroll 1
     for (int64_t i = tid; i < w.items; i += THREADS) {
       const int steps = kv8_item(a, w, i).steps;
       mine += steps ? steps + w.item_steps : 0;
@@ -238,7 +240,7 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
     if (lane == 0) sums[warp] = mine;
     __syncthreads();
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < W; ++i) total += sums[i];
     __syncthreads();
   }
@@ -248,6 +250,7 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
   }
   int64_t carry = 0, lo = 0, hi = 0, share = 1;
   int carried = 0;  // segments so far
+#pragma unroll 1
   for (int64_t base = 0; base < w.items; base += THREADS) {
     const int64_t i = base + tid;
     if (!one) {
@@ -264,7 +267,7 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
     if (lane == 31) sums[warp] = sum;
     __syncthreads();
     int64_t before = carry, all = 0;
-#pragma unroll
+#pragma unroll 4
     for (int j = 0; j < W; ++j) {
       if (j < warp) before += sums[j];
       all += sums[j];
@@ -279,7 +282,7 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
     if (lane == 0) counts[warp] = __popc(those);
     __syncthreads();
     int at = carried + __popc(those & ((1u << lane) - 1));
-#pragma unroll
+#pragma unroll 4
     for (int j = 0; j < W; ++j) {
       if (j < warp) at += counts[j];
       carried += counts[j];

@@ -3,22 +3,23 @@
 // Here the operations bound the call, 4 * D for every pair of a query and a key, and what the tensor cores do not do has to
 // fit beside them: an exponential for every pair (16 a clock on an SM, which is what the products of D = 128 take as well)
 // and the values' way from 8 bits to 16.
-//   S [128 rows x 128 keys] = (Qhi + Qlo) [128 x D] K^T [D x 128]    e4m3 codes as TMA leaves them; the queries in two terms,
-//                                                                    which together take as long as one product of bf16
-//   O [128 rows x D]       += P [128 x 128 keys] V [128 x D]         bf16: P from tensor memory, V from shared memory
+//   S [128 rows x 64 keys] = (Qhi + Qlo) [128 x D] K^T [D x 64]   e4m3 codes as TMA leaves them; the queries in two terms,
+//                                                                  which together take as long as one product of bf16
+//   O [128 rows x D]      += P [128 x 64 keys] V [64 x D]          bf16: P from tensor memory, V from shared memory
 // A query is hi = e4m3(x), lo = e4m3(x - hi), x scaled by a power of two that brings its row's largest value to 2^7 .. 2^8:
 // bf16 values stay exact unless they are below 2^-10 of that, which may lose 2^-18 of it.  The keys' scales are left to the
 // softmax, where they are part of the factor that scores are multiplied by anyhow.  The values become bf16 with their scale in
 // them, which is exact: a code has 4 significant bits, and bf16 has the range of fp32.  So weights need no more than bf16
 // either, whatever the scales of other pages are.
 //
-// An item has 256 rows, two tiles of 128 that take turns on the tensor cores: while one tile's scores go through the
-// exponentials, the other's products run, and every page that is read and turned into bf16 serves both.  An item of 128 rows or
-// fewer gives both tiles to the same rows: they take the steps of 128 keys in turn and are brought together at its end.
+// An item has 256 rows, two tiles of 128, so that every page that is read and turned into bf16 serves both.  A tile's S has
+// two buffers of a page's 64 keys: the products of a page run while the softmax is at the page before it.  (With one buffer of
+// 128 keys, products and softmax of a tile wait for each other: 1800 us instead of 1319 for 4680 x 46,800 x 12 heads.)  An item of 128
+// rows or fewer gives both tiles to the same rows: they take its pages in turn and are brought together at its end.
 //
-// Warps: 0 loads pages, 1 issues the products, 4 - 7 turn values into bf16 and, an item ahead, queries into their two terms, 8 - 11
+// Warps: 0 loads pages, 1 issues the scores' products, 2 those of the values, 4 - 7 turn values into bf16 and, an item ahead, queries into their two terms, 8 - 11
 // and 12 - 15 are the softmax of a tile each, a row to a thread.
-// Tensor memory: S of both tiles (P, packed bf16, over its first half), O of both tiles.
+// Tensor memory: four S (P, packed bf16, over their first halves), O of both tiles.
 #include "kv8.cuh"
 #include "kv8_mma.cuh"
 
@@ -27,33 +28,33 @@ namespace hsa {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kTile = 128;          // rows of a tile; keys of a step
+constexpr int kTile = 128;          // rows of a tile
 constexpr float kGrow = 8.f;        // a row's reference is set anew when a score passes it by 2^8: sums and O have room for that
-constexpr int kMetas = 8;
+constexpr int kMetas = 16;
+constexpr int kPoly = 0;
 
 template <int D>
 struct ChunkSmem {
   static constexpr int kPage = kBlock * D;
-  static constexpr int kStage = 2 * kPage;
-  static constexpr int kKStages = D == 128 ? 3 : 6, kVStages = D == 128 ? 2 : 4;
+  static constexpr int kKStages = D == 128 ? 6 : 12, kVStages = 4, kBStages = 4;  // pages
   union {
     uint8_t q[2][2][kTile * D];        // [tile][term]
     float other[D][kTile];             // O of the second tile, where both have the same rows
   };
-  uint8_t k[kKStages][kStage];
-  uint8_t vc[kVStages][kStage];        // codes
-  uint8_t vb[2][kTile * D * 2];        // bf16, [64 dims][key][64 dims], dims of a group of four in the order 0, 2, 1, 3
+  uint8_t k[kKStages][kPage];
+  uint8_t vc[kVStages][kPage];         // codes
+  uint8_t vb[kBStages][kPage * 2];     // bf16, [64 dims][key][64 dims], dims of a group of four in the order 0, 2, 1, 3
   float qscale[2 * kTile];
   float other_ref[kTile], other_sum[kTile];
-  PageMeta meta[kMetas][2];
+  PageMeta meta[kMetas];
   int last[2];
-  uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[2], vb_empty[2];
-  uint64_t s_full[2], p_full[2][2], o_done[2], q_full, q_free, other_full, done;
+  uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[kBStages], vb_empty[kBStages];
+  uint64_t s_full[4], p_full[4], pv_done[4], q_full, q_free, other_full, done[2];
   uint32_t tmem;
   Kv8Plan plan;
 };
 
-constexpr uint32_t kColS = 0, kColO = 256;  // + 128 a tile
+constexpr uint32_t kColS = 0, kColO = 256;  // + 64 a buffer of S, + 128 a tile
 
 // ---- two fp32 in a register pair
 __device__ __forceinline__ uint64_t pair(float a, float b) {
@@ -101,14 +102,14 @@ __device__ __forceinline__ uint64_t ex2_poly(uint64_t x) {
               __uint_as_float(__float_as_uint(pf.y) + (__float_as_uint(tf.y) << 23)));
 }
 
-// Weights of 32 keys: 2^(s * c - ref) as bf16 pairs, and their sums in fp32.  POLY of every 16 are polynomials.
-template <int POLY>
+// Weights of 32 keys: 2^(s * c - ref) as bf16 pairs, and their sums in fp32.  N of 16 pairs are polynomials.
+template <int N>
 __device__ __forceinline__ void weights(const uint32_t* s, float c, float nref, uint64_t* sum, uint32_t* w) {
   const uint64_t c2 = pair(c, c), r2 = pair(nref, nref);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     uint64_t y = fma2(pair(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, r2);
-    if ((i * POLY) % 16 < POLY) {
+    if ((i * N) % 16 < N) {
       y = ex2_poly(y);
     } else {
       const float2 f = unpair(y);
@@ -158,9 +159,9 @@ __device__ __forceinline__ float* part_of(const Kv8Work& w, int64_t slot, int ti
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
-kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant__ Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using Smem = ChunkSmem<D>;
-  constexpr int kKStages = Smem::kKStages, kVStages = Smem::kVStages, kPage = Smem::kPage, kStage = Smem::kStage;
+  constexpr int kKStages = Smem::kKStages, kVStages = Smem::kVStages, kBStages = Smem::kBStages, kPage = Smem::kPage;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
@@ -173,18 +174,20 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
       mbar_init(&sm.vc_full[i], 1);
       mbar_init(&sm.vc_empty[i], 4);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kBStages; ++i) {
       mbar_init(&sm.vb_full[i], 4);
       mbar_init(&sm.vb_empty[i], 1);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&sm.s_full[i], 1);
-      mbar_init(&sm.p_full[i][0], 4);
-      mbar_init(&sm.p_full[i][1], 4);
-      mbar_init(&sm.o_done[i], 1);
+      mbar_init(&sm.p_full[i], 4);
+      mbar_init(&sm.pv_done[i], 1);
     }
     mbar_init(&sm.q_full, 4);
     mbar_init(&sm.q_free, 1 + 8);  // its products, and the softmax warps (scales; the merge of two tiles)
     mbar_init(&sm.other_full, 4);
-    mbar_init(&sm.done, 1);
+    mbar_init(&sm.done[0], 1);
+    mbar_init(&sm.done[1], 1);
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -203,10 +206,7 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
   Kv8Walk walk;
   bool ok = true;  // false: a wait ran out; nothing more is waited for
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok && !mbar_wait(bar, parity)) {
-      ok = false;
-      kv8_flag(a.status, kDevTimeout);
-    }
+    if (ok) ok = mbar_wait_short(bar, parity);
     return ok;
   };
   // the same for a whole warp that stays together
@@ -219,41 +219,34 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 0) {
-      // ---- loads.  The lanes look up the pages of 16 steps at once.
+      // ---- loads.  The lanes look up 32 pages at once.
       uint32_t n = 0;
       while (ok && walk.next(a, w, sm.plan)) {
         const Kv8Item& it = walk.g.it;
-        const int per = shared_rows(it) ? 2 : 1, s1 = walk.g.s1 * per;  // steps of 128 keys
-        for (int s = walk.g.s0 * per; s < s1 && ok; s += 16) {
+        const int per = shared_rows(it) ? 2 : 1, s1 = walk.g.s1 * per;  // pages
+        for (int s = walk.g.s0 * per; s < s1 && ok; s += 32) {
           int blk = 0, page = -1;
           PageMeta meta{-1, 1.f, 0.f};
-          if (s + lane / 2 < s1) page = kv8_page(a, it, s * 2 + lane, &blk);
+          if (s + lane < s1) page = kv8_page(a, it, s + lane, &blk);
           if (page >= 0) {
             const int64_t ph = static_cast<int64_t>(page) * a.Hkv + it.h;
             meta.pos = blk * kBlock;
             meta.ks = __ldg(a.k_scale + ph);
             meta.vs = __ldg(a.v_scale + ph);
           }
-          const int count = min(16, s1 - s);
+          const int count = min(32, s1 - s);
+#pragma unroll 1
           for (int i = 0; i < count; ++i, ++n) {
             const uint32_t st = n % kKStages, sv = n % kVStages;
             if (!warp_wait(&sm.k_empty[st], ((n / kKStages) & 1) ^ 1)) break;
-            int pages[2], bytes = 0;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              pages[j] = __shfl_sync(0xffffffffu, page, i * 2 + j);
-              if (pages[j] >= 0) bytes += kPage;
-            }
+            const int p = __shfl_sync(0xffffffffu, page, i);
+            const int row = static_cast<int>((static_cast<int64_t>(p) * a.Hkv + it.h) * kBlock);
             // the loads go out before the scales are there; the barrier is arrived at behind them
-            if (elect_one_sync()) {
-              if (bytes) mbar_expect_tx_only(&sm.k_full[st], bytes);
-#pragma unroll
-              for (int j = 0; j < 2; ++j)
-                if (pages[j] >= 0)
-                  tma_load_2d(sm.k[st] + j * kPage, &tm_k, &sm.k_full[st], 0,
-                              static_cast<int>((static_cast<int64_t>(pages[j]) * a.Hkv + it.h) * kBlock));
+            if (p >= 0 && elect_one_sync()) {
+              mbar_expect_tx_only(&sm.k_full[st], kPage);
+              tma_load_2d(sm.k[st], &tm_k, &sm.k_full[st], 0, row);
             }
-            if (lane / 2 == i) sm.meta[n % kMetas][lane % 2] = meta;
+            if (lane == i) sm.meta[n % kMetas] = meta;
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.k_full[st]);
             if (!warp_wait(&sm.vc_empty[sv], ((n / kVStages) & 1) ^ 1)) {
@@ -262,80 +255,84 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
               break;
             }
             if (elect_one_sync()) {
-              if (bytes) mbar_expect_tx(&sm.vc_full[sv], bytes);
-              else mbar_arrive(&sm.vc_full[sv]);
-#pragma unroll
-              for (int j = 0; j < 2; ++j)
-                if (pages[j] >= 0)
-                  tma_load_2d(sm.vc[sv] + j * kPage, &tm_v, &sm.vc_full[sv], 0,
-                              static_cast<int>((static_cast<int64_t>(pages[j]) * a.Hkv + it.h) * kBlock));
+              if (p >= 0) {
+                mbar_expect_tx(&sm.vc_full[sv], kPage);
+                tma_load_2d(sm.vc[sv], &tm_v, &sm.vc_full[sv], 0, row);
+              } else {
+                mbar_arrive(&sm.vc_full[sv]);
+              }
             }
             __syncwarp();
           }
         }
       }
       if (!ok) {  // pages that nobody took: their loads must not outlive the CTA
-        for (uint32_t i = 1; i <= kKStages && i <= n; ++i) mbar_wait(&sm.k_full[(n - i) % kKStages], ((n - i) / kKStages) & 1);
-        for (uint32_t i = 1; i <= kVStages && i <= n; ++i) mbar_wait(&sm.vc_full[(n - i) % kVStages], ((n - i) / kVStages) & 1);
+        for (uint32_t i = 1; i <= kKStages && i <= n; ++i) mbar_wait_short(&sm.k_full[(n - i) % kKStages], ((n - i) / kKStages) & 1);
+        for (uint32_t i = 1; i <= kVStages && i <= n; ++i) mbar_wait_short(&sm.vc_full[(n - i) % kVStages], ((n - i) / kVStages) & 1);
       }
     } else if (warp == 1) {
-      // ---- products
+      // ---- scores.  Unit u of an item: tile u % 2 and a page; units are counted through, and have the buffers of S in turn.
       if (elect_one_sync()) {
-        constexpr uint32_t id_s = idesc_e4m3(128, 128, 0, 0), id_o = idesc_bf16_f32(128, D, 0, 1), hi_v = desc_hi_sw128(1024);
+        constexpr uint32_t id = idesc_e4m3(128, kBlock, 0, 0);
         const uint64_t q0 = row_desc<D>(smem_u32(sm.q), 0), k0 = row_desc<D>(smem_u32(sm.k), 0);
-        const uint32_t v0 = desc_lo_sw128(smem_u32(sm.vb), kTile * 128);
-        uint32_t items = 0, nk = 0, nv = 0, np[2] = {0, 0};  // items; steps whose keys, values have been seen; weights of a tile
+        uint32_t items = 0, n = 0, st = 0, round = 0;
         while (ok && walk.next(a, w, sm.plan)) {
           const bool same = shared_rows(walk.g.it);
-          const int units = 2 * (walk.g.s1 - walk.g.s0);  // unit u: tile u % 2 at its next step
-          if (!wait(&sm.q_full, items & 1)) break;
-          const auto scores = [&](int u) {
-            const int t = u & 1;
-            const uint32_t st = nk % kKStages;
-            if (same || t == 0) {
-              if (!wait(&sm.k_full[st], (nk / kKStages) & 1)) return;
-              tc_fence_after();
-            }
-            const uint64_t q = q0 + ((same ? 0 : t) * 2 * kTile * D) / 16, k = k0 + (st * kStage) / 16;
+          const int units = 2 * (walk.g.s1 - walk.g.s0);
+          if (!wait(&sm.q_full, items++ & 1)) break;
+#pragma unroll 1
+          for (int u = 0; u < units; ++u, ++n) {
+            const uint32_t t = n & 1, b = n & 3;
+            if (!wait(&sm.k_full[st], round & 1) || !wait(&sm.pv_done[b], ((n / 4) & 1) ^ 1)) break;
+            tc_fence_after();
+            const uint64_t q = q0 + ((same ? 0 : t) * 2 * kTile * D) / 16, k = k0 + (st * kPage) / 16;
 #pragma unroll
             for (int term = 0; term < 2; ++term)
 #pragma unroll
               for (int kk = 0; kk < D / 32; ++kk)
-                mma_f8(tmem + kColS + t * 128, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, id_s, term + kk > 0);
-            tc_commit(&sm.s_full[t]);
+                mma_f8(tmem + kColS + b * 64, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, id, term + kk > 0);
+            tc_commit(&sm.s_full[b]);
             if (same || t == 1) {
               tc_commit(&sm.k_empty[st]);
-              ++nk;
+              if (++st == kKStages) {
+                st = 0;
+                ++round;
+              }
             }
-            if (u == units - 1) tc_commit(&sm.q_free);
-          };
-          scores(0);
-          scores(1);
-          for (int u = 0; u < units && ok; ++u) {
-            const int t = u & 1;
-            const uint32_t b = nv & 1;
-            const uint32_t v = v0 + (b * (kTile * D * 2)) / 16;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              if (!wait(&sm.p_full[t][half], np[t] & 1)) break;
-              if (half == 0 && (same || t == 0) && !wait(&sm.vb_full[b], (nv / 2) & 1)) break;
-              tc_fence_after();
-#pragma unroll
-              for (int kk = half * 4; kk < half * 4 + 4; ++kk)
-                tc_mma_ts_lo(tmem + kColO + t * 128, tmem + kColS + t * 128 + kk * 8, v + kk * 128, hi_v, id_o, u >= 2 || kk > 0);
-            }
-            ++np[t];
-            if (same || t == 1) {
-              tc_commit(&sm.vb_empty[b]);
-              ++nv;
-            }
-            if (u >= units - 2) tc_commit(&sm.o_done[t]);
-            if (u + 2 < units && ok) scores(u + 2);
           }
-          ++items;
+          tc_commit(&sm.q_free);
         }
-        tc_commit(&sm.done);
-        mbar_wait(&sm.done, 0);
+        tc_commit(&sm.done[0]);
+        ok &= mbar_wait_short(&sm.done[0], 0);
+      }
+      __syncwarp();
+    } else if (warp == 2) {
+      // ---- values
+      if (elect_one_sync()) {
+        constexpr uint32_t id = idesc_bf16_f32(128, D, 0, 1), hi = desc_hi_sw128(1024);
+        const uint32_t v0 = desc_lo_sw128(smem_u32(sm.vb), kBlock * 128);
+        uint32_t n = 0, pages = 0;
+        while (ok && walk.next(a, w, sm.plan)) {
+          const bool same = shared_rows(walk.g.it);
+          const int units = 2 * (walk.g.s1 - walk.g.s0);
+#pragma unroll 1
+          for (int u = 0; u < units; ++u, ++n) {
+            const uint32_t t = n & 1, b = n & 3, sv = pages % kBStages;
+            if (!wait(&sm.p_full[b], (n / 4) & 1) || !wait(&sm.vb_full[sv], (pages / kBStages) & 1)) break;
+            tc_fence_after();
+            const uint32_t v = v0 + (sv * (kPage * 2)) / 16;
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              tc_mma_ts_lo(tmem + kColO + t * 128, tmem + kColS + b * 64 + kk * 8, v + kk * 128, hi, id, u >= 2 || kk > 0);
+            tc_commit(&sm.pv_done[b]);
+            if (same || t == 1) {
+              tc_commit(&sm.vb_empty[sv]);
+              ++pages;
+            }
+          }
+        }
+        tc_commit(&sm.done[1]);
+        ok &= mbar_wait_short(&sm.done[1], 0);
       }
       __syncwarp();
     }
@@ -351,6 +348,7 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
         const int r0 = c / V, e = c % V;
         const int rows = shared_rows(it) ? kTile : 2 * kTile;
         bool waited = false;
+#pragma unroll 1
         for (int base = 0; base < rows; base += R * kAtOnce) {
           uint4 in[kAtOnce];
 #pragma unroll
@@ -402,44 +400,41 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
         if (lane == 0) mbar_arrive(&sm.q_full);
         ++items;
       }
-      const int steps = (walk.g.s1 - walk.g.s0) * (shared_rows(it) ? 2 : 1);
+      const int pages = (walk.g.s1 - walk.g.s0) * (shared_rows(it) ? 2 : 1);
       constexpr int C = D / 16, R = 128 / C;  // 16 dims of a row, rows at a time
       const int r0 = c / C, e = c % C;
-      for (int s = 0; s < steps; ++s, ++n) {
-        const uint32_t sv = n % kVStages, b = n & 1;
+#pragma unroll 1
+      for (int s = 0; s < pages; ++s, ++n) {
+        const uint32_t sv = n % kVStages, b = n % kBStages;
         warp_wait(&sm.vc_full[sv], (n / kVStages) & 1);
-        warp_wait(&sm.vb_empty[b], ((n / 2) & 1) ^ 1);
-        uint8_t* to = sm.vb[b] + (e / 4) * (kTile * 128);
+        uint4 in[kBlock / R];
 #pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-          const float vs = sm.meta[n % kMetas][pg].vs;
-          // 2^120 vs, in one factor where it fits
-          const bool two = vs > 64.f;
-          const float f1 = two ? 0x1p120f : vs * 0x1p60f * 0x1p60f;
-          const uint32_t m1 = pack_bf16(f1, f1), m2 = pack_bf16(vs, vs);
-          const uint8_t* from = sm.vc[sv] + pg * kPage;
-          uint4 in[kBlock / R];
+        for (int i = 0; i < kBlock / R; ++i) in[i] = *reinterpret_cast<const uint4*>(sm.vc[sv] + swizzled<D>(i * R + r0, e * 16));
+        const float vs = sm.meta[n % kMetas].vs;
+        // 2^120 vs, in one factor where it fits
+        const bool two = vs > 64.f;
+        const float f1 = two ? 0x1p120f : vs * 0x1p60f * 0x1p60f;
+        const uint32_t m1 = pack_bf16(f1, f1), m2 = pack_bf16(vs, vs);
+        warp_wait(&sm.vb_empty[b], ((n / kBStages) & 1) ^ 1);
+        uint8_t* to = sm.vb[b] + (e / 4) * (kBlock * 128);
 #pragma unroll
-          for (int i = 0; i < kBlock / R; ++i) in[i] = *reinterpret_cast<const uint4*>(from + swizzled<D>(i * R + r0, e * 16));
+        for (int i = 0; i < kBlock / R; ++i) {
+          const int row = i * R + r0;
+          uint4 out[2];
+          codes_to_bf16(in[i].x, m1, &out[0].x, &out[0].y);
+          codes_to_bf16(in[i].y, m1, &out[0].z, &out[0].w);
+          codes_to_bf16(in[i].z, m1, &out[1].x, &out[1].y);
+          codes_to_bf16(in[i].w, m1, &out[1].z, &out[1].w);
+          if (__builtin_expect(two, 0)) {
 #pragma unroll
-          for (int i = 0; i < kBlock / R; ++i) {
-            const int row = pg * kBlock + i * R + r0;
-            uint4 out[2];
-            codes_to_bf16(in[i].x, m1, &out[0].x, &out[0].y);
-            codes_to_bf16(in[i].y, m1, &out[0].z, &out[0].w);
-            codes_to_bf16(in[i].z, m1, &out[1].x, &out[1].y);
-            codes_to_bf16(in[i].w, m1, &out[1].z, &out[1].w);
-            if (two) {
-#pragma unroll
-              for (int j = 0; j < 2; ++j)
-                out[j] = make_uint4(mul_bf16x2(out[j].x, m2), mul_bf16x2(out[j].y, m2), mul_bf16x2(out[j].z, m2), mul_bf16x2(out[j].w, m2));
-            }
-            // (lanes of the upper slab store their second half first: no two of eight lanes meet in a bank)
-            const bool flip = (e & 4) != 0;
-            const int c0 = (e & 3) * 2;
-            *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 1 : 0)) ^ (row & 7)) << 4)) = flip ? out[1] : out[0];
-            *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 0 : 1)) ^ (row & 7)) << 4)) = flip ? out[0] : out[1];
+            for (int j = 0; j < 2; ++j)
+              out[j] = make_uint4(mul_bf16x2(out[j].x, m2), mul_bf16x2(out[j].y, m2), mul_bf16x2(out[j].z, m2), mul_bf16x2(out[j].w, m2));
           }
+          // (lanes of the upper slab store their second half first: no two of eight lanes meet in a bank)
+          const bool flip = (e & 4) != 0;
+          const int c0 = (e & 3) * 2;
+          *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 1 : 0)) ^ (row & 7)) << 4)) = flip ? out[1] : out[0];
+          *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 0 : 1)) ^ (row & 7)) << 4)) = flip ? out[0] : out[1];
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -455,8 +450,8 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
     // because they meet at barriers; the status word says that the result is none.
     const int t = (warp - 8) / 4, r = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t col_s = tmem + lanes + kColS + t * 128, col_o = tmem + lanes + kColO + t * 128;
-    uint32_t items = 0, n = 0, kn = 0, merges = 0;  // items, units of this tile, steps of 128 keys before the item's first
+    const uint32_t col_o = tmem + lanes + kColO + t * 128;
+    uint32_t items = 0, n = 0, kn = 0, merges = 0;  // items, units of this tile, pages before the item's first
     Kv8Segment cut0, cut1;  // of the items that the run shares with others: its first and its last
     int n_cut = 0;
     while (walk.next(a, w, sm.plan)) {
@@ -474,46 +469,45 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
       }
       float ref = kNone;
       uint64_t sum[2] = {0, 0};
+#pragma unroll 1
       for (int u = 0; u < units; ++u, ++n) {
-        const PageMeta* meta = sm.meta[(kn + (same ? 2 * u + t : u)) % kMetas];
-        wait(&sm.s_full[t], n & 1);
+        const uint32_t b = (n & 1) * 2 + t, col_s = tmem + lanes + kColS + b * 64;
+        wait(&sm.s_full[b], (n / 2) & 1);
         __syncwarp();
         tc_fence_after();
-        uint32_t x[128];
+        uint32_t x[64];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(col_s + i * 32, *reinterpret_cast<uint32_t(*)[32]>(x + i * 32));
-        const int pos0 = meta[0].pos, pos1 = meta[1].pos;
-        const float c0 = fmaxf(qs * meta[0].ks, 0x1p-126f), c1 = fmaxf(qs * meta[1].ks, 0x1p-126f);  // (never 0: scores may be -inf)
-        const bool masked = min(pos0, pos1) < 0 || max(pos0, pos1) + kBlock > lim_low;
+        for (int i = 0; i < 2; ++i) tmem_ld32(col_s + i * 32, *reinterpret_cast<uint32_t(*)[32]>(x + i * 32));
+        const PageMeta meta = sm.meta[(kn + (same ? 2 * u + t : u)) % kMetas];
+        const float c = fmaxf(qs * meta.ks, 0x1p-126f);  // (never 0: scores may be -inf)
+        const bool masked = meta.pos < 0 || meta.pos + kBlock > lim_low;
         tc_wait_ld();
-        if (masked) {
-          const int lim0 = pos0 < 0 ? 0 : lim - pos0, lim1 = pos1 < 0 ? 0 : lim - pos1;
+        if (__builtin_expect(masked, 0)) {
+          const int lim0 = meta.pos < 0 ? 0 : lim - meta.pos;
 #pragma unroll
-          for (int i = 0; i < 64; ++i) {
+          for (int i = 0; i < 64; ++i)
             if (i >= lim0) x[i] = 0xff800000u;
-            if (i >= lim1) x[64 + i] = 0xff800000u;
-          }
         }
         float top;
         {
           float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 64; i += 4) {
-            m[0] = max3(m[0], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-            m[1] = max3(m[1], __uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
-            m[2] = max3(m[2], __uint_as_float(x[64 + i]), __uint_as_float(x[64 + i + 1]));
-            m[3] = max3(m[3], __uint_as_float(x[64 + i + 2]), __uint_as_float(x[64 + i + 3]));
+          for (int i = 0; i < 64; i += 8) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m[j] = max3(m[j], __uint_as_float(x[i + 2 * j]), __uint_as_float(x[i + 2 * j + 1]));
           }
-          top = fmaxf(fmaxf(m[0], m[1]) * c0, fmaxf(m[2], m[3]) * c1);
+          top = max3(fmaxf(m[0], m[1]), m[2], m[3]) * c;
         }
-        if (__any_sync(0xffffffffu, top > ref + kGrow)) {
+        if (__builtin_expect(__any_sync(0xffffffffu, top > ref + kGrow), 0)) {
           const float to = top > ref + kGrow ? top : ref, f = ex2(ref - to);
           ref = to;
           const uint64_t f2 = pair(f, f);
           sum[0] = fma2(sum[0], f2, 0);
           sum[1] = fma2(sum[1], f2, 0);
-          // (the scores came behind the products before them: O is at rest)
           if (u > 0) {
+            wait(&sm.pv_done[((n - 1) & 1) * 2 + t], ((n - 1) / 2) & 1);  // (those before have been, or these scores were not there)
+            __syncwarp();
+            tc_fence_after();
 #pragma unroll 1
             for (int i = 0; i < D; i += 16) {
               uint32_t o[16];
@@ -525,28 +519,19 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
             }
           }
         }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const float c = half ? c1 : c0;
-          uint32_t p[32];
-          if (masked) {
-            weights<0>(x + half * 64, c, -ref, sum, p);
-            weights<0>(x + half * 64 + 32, c, -ref, sum, p + 16);
-          } else {
-            weights<4>(x + half * 64, c, -ref, sum, p);
-            weights<4>(x + half * 64 + 32, c, -ref, sum, p + 16);
-          }
-          tmem_st32(col_s + half * 32, p);
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.p_full[t][half]);
-        }
+        uint32_t p[32];
+        weights<kPoly>(x, c, -ref, sum, p);
+        weights<kPoly>(x + 32, c, -ref, sum, p + 16);
+        tmem_st32(col_s, p);
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm.p_full[b]);
       }
       kn += units * (same ? 2 : 1);
       const float2 s0 = unpair(sum[0]), s1 = unpair(sum[1]);
       float l = (s0.x + s0.y) + (s1.x + s1.y);
-      wait(&sm.o_done[t], items & 1);
+      wait(&sm.pv_done[((n - 1) & 1) * 2 + t], ((n - 1) / 2) & 1);
       __syncwarp();
       tc_fence_after();
       ++items;
@@ -627,6 +612,7 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
       }
     }
     // ---- items that other CTAs have parts of: the last one to get here joins them
+#pragma unroll 1
     for (int i = 0; i < n_cut; ++i) {
       const Kv8Segment g = i == 0 ? cut0 : cut1;
       tile_sync(t);
@@ -645,16 +631,19 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
       const int row = shared_rows(g.it) ? r : t * kTile + r;
       if (sm.last[t] && row < g.it.rows) {
         float m = kNone;
+#pragma unroll 1
         for (int j = g.first_cta; j <= g.last_cta; ++j)
           m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
         const int at = g.it.row0 + row, head = g.it.h * a.group + at % a.group;
         const int64_t tok = g.it.first + at / a.group;
         float l = 0.f;
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {
           float4 o[D / 8];
 #pragma unroll
           for (int k = 0; k < D / 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
           l = 0.f;
+#pragma unroll 1
           for (int j = g.first_cta; j <= g.last_cta; ++j) {
             const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t);
             const float f = ex2(__ldcg(p + kTile * D + r) - m);
@@ -678,6 +667,7 @@ kv8_chunk_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__
       }
     }
   }
+  if (!ok) kv8_flag(a.status, kDevTimeout);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -705,10 +695,10 @@ cudaError_t launch_kv8_chunk(const Kv8AttendArgs& a, Kv8Work w, int D, int ctas,
   w.tile_rows = 2 * kTile;
   w.tiles = static_cast<int>((rows + 2 * kTile - 1) / (2 * kTile));
   w.items = static_cast<int64_t>(a.rows.batch) * a.Hkv * w.tiles;
-  w.step_pages = 2;
+  w.step_pages = 1;
   w.half_rows = kTile;
-  w.min_steps = 4;
-  w.item_steps = 2;
+  w.min_steps = 8;
+  w.item_steps = 4;
   w.slot_floats = static_cast<int64_t>(kv8_chunk_slot(D));
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(ctas);

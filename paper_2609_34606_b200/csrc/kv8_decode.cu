@@ -162,7 +162,7 @@ __device__ __forceinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work
 
 template <int D, int R>
 __global__ void __launch_bounds__((DecodeShape<D, R>::kThreads), 1)
-kv8_decode_kernel(const Kv8AttendArgs a, const Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant__ Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using Sh = DecodeShape<D, R>;
   using Smem = DecodeSmem<D, R>;
   constexpr int N = Sh::N, kStages = Sh::kStages, kGroups = Sh::kGroups;
