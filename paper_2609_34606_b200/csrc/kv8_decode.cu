@@ -54,6 +54,7 @@ struct DecodeSmem {
   uint8_t q[2][Sh::N * D];
   float other[Sh::kGroups == 2 ? R * (D + 2) : 1];  // sums of the group that does not write the item: [R][D], references, sums of weights
   float qscale[2][R];
+  int limit[2][R];                         // tokens that a row sees
   PageMeta meta[Sh::kStages][2];
   float red[Sh::kGroups][4][R];
   uint64_t k_full[Sh::kStages], v_full[Sh::kStages], empty[Sh::kStages];
@@ -204,10 +205,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
   Kv8Walk walk;
   bool ok = true;  // false: a wait ran out; nothing more is waited for
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok && !mbar_wait(bar, parity)) {
-      ok = false;
-      kv8_flag(a.status, kDevTimeout);
-    }
+    if (ok) ok = mbar_wait_short(bar, parity);
     return ok;
   };
   // the same for a whole warp that stays together
@@ -229,6 +227,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
           meta.vs = __ldg(a.v_scale + ph);
         }
         const int count = min(16, walk.g.s1 - s);
+#pragma unroll 1
         for (int i = 0; i < count; ++i, ++n) {
           const uint32_t st = n % kStages;
           if (!warp_wait(&sm.empty[st], ((n / kStages) & 1) ^ 1)) break;
@@ -262,8 +261,8 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
     }
     if (!ok)  // pages that nobody took: their loads must not outlive the CTA
       for (uint32_t i = 1; i <= kStages && i <= n; ++i) {
-        mbar_wait(&sm.k_full[(n - i) % kStages], ((n - i) / kStages) & 1);
-        mbar_wait(&sm.v_full[(n - i) % kStages], ((n - i) / kStages) & 1);
+        mbar_wait_short(&sm.k_full[(n - i) % kStages], ((n - i) / kStages) & 1);
+        mbar_wait_short(&sm.v_full[(n - i) % kStages], ((n - i) / kStages) & 1);
       }
   } else if (warp == 1) {
     // ---- first products
@@ -274,6 +273,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
       while (ok && walk.next(a, w, sm.plan)) {
         const uint32_t qb = items & 1;
         if (!wait(&sm.q_full[qb], (items / 2) & 1)) break;
+#pragma unroll 1
         for (int s = walk.g.s0; s < walk.g.s1; ++s, ++n) {
           const uint32_t b = n & 1;
           if (!wait(&sm.k_full[st], round & 1) || !wait(&sm.s_free[b], ((n / 2) & 1) ^ 1)) break;
@@ -291,7 +291,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         ++items;
       }
       tc_commit(&sm.done[0]);
-      mbar_wait(&sm.done[0], 0);
+      mbar_wait_short(&sm.done[0], 0);
     }
     __syncwarp();
   } else if (warp == 3) {
@@ -303,6 +303,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
       const uint64_t v0 = row_desc<D>(smem_u32(sm.v), D == 128 ? 0 : Sh::kPage), p0 = row_desc<128>(smem_u32(sm.p), 0);
       uint32_t n = 0, st = 0, round = 0;
       while (ok && walk.next(a, w, sm.plan)) {
+#pragma unroll 1
         for (int s = walk.g.s0; s < walk.g.s1; ++s, ++n) {
           const uint32_t b = n & 1;
           if (!wait(&sm.p_full[b], (n / 2) & 1) || !wait(&sm.v_full[st], round & 1)) break;
@@ -324,7 +325,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         }
       }
       tc_commit(&sm.done[1]);
-      mbar_wait(&sm.done[1], 0);
+      mbar_wait_short(&sm.done[1], 0);
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -348,6 +349,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
       }
       if (!warp_wait(&sm.q_free[qb], ((items / 2) & 1) ^ 1)) break;
       uint8_t* q = sm.q[qb];
+      if (lane < R) sm.limit[qb][lane] = it.limit(a, min(lane, it.rows - 1));
 #pragma unroll
       for (int i = 0; i < kTimes; ++i) {
         const int r = r0 + i * kRows;
@@ -427,6 +429,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         added = i + kGroups;
       };
       wait(&sm.q_full[qb], ((items - 1) / 2) & 1);
+#pragma unroll 1
       for (; j < end; j += kGroups) {
         const uint32_t st = j % kStages, b = j & 1;
         wait(&sm.s_full[b], (j / 2) & 1);
@@ -448,7 +451,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
           } else if (pos >= lim_low) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
-              if (pos >= it.limit(a, min(r, rows - 1))) y[r] = -INFINITY;
+              if (pos >= sm.limit[qb][r]) y[r] = -INFINITY;
           }
 #pragma unroll
           for (int r = 0; r < R; ++r) over |= y[r] > ref[r] + kSlack;
@@ -456,7 +459,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         const float vs0_now = sm.meta[st][0].vs, vs1_now = sm.meta[st][1].vs;
         tc_fence_before();
         mbar_arrive(&sm.s_free[b]);
-        if (group_any(group, over)) {
+        if (__builtin_expect(group_any(group, over), 0)) {
           // the maxima anew
           if (added < j) add(added);
 #pragma unroll
@@ -589,6 +592,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
       group_sync(group);
     }
   }
+  if (!ok) kv8_flag(a.status, kDevTimeout);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
