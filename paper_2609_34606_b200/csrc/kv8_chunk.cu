@@ -29,9 +29,8 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kTile = 128;          // rows of a tile
-constexpr float kGrow = 8.f;        // a row's reference is set anew when a score passes it by 2^8: sums and O have room for that
+constexpr float kMost = 8192.f;     // weights of a page's 64 keys may add up to this before a row's reference is set anew: sums and O have room for that
 constexpr int kMetas = 16;
-constexpr int kPoly = 0;
 
 template <int D>
 struct ChunkSmem {
@@ -48,6 +47,7 @@ struct ChunkSmem {
   float other_ref[kTile], other_sum[kTile];
   PageMeta meta[kMetas];
   int last[2];
+  Kv8Segment cut[2][2];                // [tile]: of the items that the run shares with others, its first and its last
   uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[kBStages], vb_empty[kBStages];
   uint64_t s_full[4], p_full[4], pv_done[4], q_full, q_free, other_full, done[2];
   uint32_t tmem;
@@ -83,42 +83,25 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return m;
 }
 
-// 2^x of a pair without the special function unit: x = n + f, |f| <= 1/2, by adding and taking away 1.5 * 2^23; 2^f as the
-// polynomial of degree 4 with p(0) = 1 whose relative error, 2.9e-6, is least on that interval (found by linear programming);
-// n goes into the exponent.  Values below 2^-126 come out as that.
-__device__ __forceinline__ uint64_t ex2_poly(uint64_t x) {
-  float2 v = unpair(x);
-  const uint64_t y = pair(fmaxf(v.x, -126.f), fmaxf(v.y, -126.f));
-  const uint64_t magic = pair(12582912.f, 12582912.f), minus = pair(-12582912.f, -12582912.f);
-  const uint64_t t = add2(y, magic);
-  const uint64_t f = fma2(add2(t, minus), pair(-1.f, -1.f), y);
-  uint64_t p = pair(0.009582576647f, 0.009582576647f);
-  p = fma2(p, f, pair(0.05590682995f, 0.05590682995f));
-  p = fma2(p, f, pair(0.2402410727f, 0.2402410727f));
-  p = fma2(p, f, pair(0.6931241184f, 0.6931241184f));
-  p = fma2(p, f, pair(1.f, 1.f));
-  const float2 pf = unpair(p), tf = unpair(t);
-  return pair(__uint_as_float(__float_as_uint(pf.x) + (__float_as_uint(tf.x) << 23)),
-              __uint_as_float(__float_as_uint(pf.y) + (__float_as_uint(tf.y) << 23)));
-}
-
-// Weights of 32 keys: 2^(s * c - ref) as bf16 pairs, and their sums in fp32.  N of 16 pairs are polynomials.
-template <int N>
-__device__ __forceinline__ void weights(const uint32_t* s, float c, float nref, uint64_t* sum, uint32_t* w) {
+// Weights of 64 keys: 2^(s * c + nref) as bf16 pairs, and their sum in fp32.  The order of the instructions is made by hand: a
+// pair's exponentials come kLag pairs behind its product, its sum and rounding another kLag behind them, so that nothing waits
+// for its operands (the compiler's order leaves a lone warp waiting at each of them).
+constexpr int kLag = 4;
+__device__ __forceinline__ float weights(uint32_t* s, float c, float nref, uint32_t* w) {
   const uint64_t c2 = pair(c, c), r2 = pair(nref, nref);
+  uint64_t sum[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    uint64_t y = fma2(pair(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, r2);
-    if ((i * N) % 16 < N) {
-      y = ex2_poly(y);
-    } else {
-      const float2 f = unpair(y);
-      y = pair(ex2(f.x), ex2(f.y));
-    }
-    sum[i & 1] = add2(sum[i & 1], y);
-    const float2 f = unpair(y);
-    w[i] = pack_bf16(f.x, f.y);
+  for (int i = 0; i < 32 + 2 * kLag; ++i) {
+    if (i < 32)
+      asm volatile("{\n.reg .b64 t;\nmov.b64 t, {%0, %1};\nfma.rn.f32x2 t, t, %2, %3;\nmov.b64 {%0, %1}, t;\n}\n" : "+r"(s[2 * i]), "+r"(s[2 * i + 1]) : "l"(c2), "l"(r2));
+    const int j = i - kLag;
+    if (j >= 0 && j < 32) asm volatile("ex2.approx.ftz.f32 %0, %0;\nex2.approx.ftz.f32 %1, %1;\n" : "+r"(s[2 * j]), "+r"(s[2 * j + 1]));
+    const int k = i - 2 * kLag;
+    if (k >= 0)
+      asm volatile("{\n.reg .b64 t;\nmov.b64 t, {%2, %3};\nadd.rn.f32x2 %0, %0, t;\ncvt.rn.bf16x2.f32 %1, %3, %2;\n}\n" : "+l"(sum[k & 1]), "=r"(w[k]) : "r"(s[2 * k]), "r"(s[2 * k + 1]));
   }
+  const float2 a = unpair(sum[0]), b = unpair(sum[1]);
+  return (a.x + a.y) + (b.x + b.y);
 }
 
 // Four e4m3 codes as bf16: (0, 2) and (1, 3).  A code's bits, put where bf16 has them, are the value times 2^-120, subnormal
@@ -204,10 +187,11 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
   Kv8Walk walk;
+  uint32_t tries = 0;
   bool ok = true;  // false: a wait ran out; nothing more is waited for
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok) ok = mbar_wait_short(bar, parity);
-    return ok;
+    tries = mbar_poll(bar, parity, tries);
+    return ok = tries == 0;
   };
   // the same for a whole warp that stays together
   const auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
@@ -267,14 +251,14 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         }
       }
       if (!ok) {  // pages that nobody took: their loads must not outlive the CTA
-        for (uint32_t i = 1; i <= kKStages && i <= n; ++i) mbar_wait_short(&sm.k_full[(n - i) % kKStages], ((n - i) / kKStages) & 1);
-        for (uint32_t i = 1; i <= kVStages && i <= n; ++i) mbar_wait_short(&sm.vc_full[(n - i) % kVStages], ((n - i) / kVStages) & 1);
+        for (uint32_t i = 1; i <= kKStages && i <= n; ++i) mbar_poll(&sm.k_full[(n - i) % kKStages], ((n - i) / kKStages) & 1, 0);
+        for (uint32_t i = 1; i <= kVStages && i <= n; ++i) mbar_poll(&sm.vc_full[(n - i) % kVStages], ((n - i) / kVStages) & 1, 0);
       }
     } else if (warp == 1) {
       // ---- scores.  Unit u of an item: tile u % 2 and a page; units are counted through, and have the buffers of S in turn.
       if (elect_one_sync()) {
         constexpr uint32_t id = idesc_e4m3(128, kBlock, 0, 0);
-        const uint64_t q0 = row_desc<D>(smem_u32(sm.q), 0), k0 = row_desc<D>(smem_u32(sm.k), 0);
+        const uint32_t q0 = row_desc_lo(smem_u32(sm.q)), k0 = row_desc_lo(smem_u32(sm.k));
         uint32_t items = 0, n = 0, st = 0, round = 0;
         while (ok && walk.next(a, w, sm.plan)) {
           const bool same = shared_rows(walk.g.it);
@@ -283,27 +267,26 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
 #pragma unroll 1
           for (int u = 0; u < units; ++u, ++n) {
             const uint32_t t = n & 1, b = n & 3;
-            if (!wait(&sm.k_full[st], round & 1) || !wait(&sm.pv_done[b], ((n / 4) & 1) ^ 1)) break;
+            wait(&sm.k_full[st], round & 1);
+            wait(&sm.pv_done[b], ((n / 4) & 1) ^ 1);
             tc_fence_after();
-            const uint64_t q = q0 + ((same ? 0 : t) * 2 * kTile * D) / 16, k = k0 + (st * kPage) / 16;
+            const uint32_t q = q0 + (same ? 0 : t) * (2 * kTile * D / 16), k = k0 + st * (kPage / 16);
 #pragma unroll
             for (int term = 0; term < 2; ++term)
 #pragma unroll
               for (int kk = 0; kk < D / 32; ++kk)
-                mma_f8(tmem + kColS + b * 64, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, id, term + kk > 0);
+                mma_f8_lo(tmem + kColS + b * 64, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, row_desc_hi<D>(), id, term + kk > 0);
             tc_commit(&sm.s_full[b]);
-            if (same || t == 1) {
-              tc_commit(&sm.k_empty[st]);
-              if (++st == kKStages) {
-                st = 0;
-                ++round;
-              }
-            }
+            const bool last = same || t == 1;  // of the page
+            tc_commit_if(&sm.k_empty[st], last);
+            st += last;
+            round += st == kKStages;
+            st = st == kKStages ? 0 : st;
           }
           tc_commit(&sm.q_free);
         }
         tc_commit(&sm.done[0]);
-        ok &= mbar_wait_short(&sm.done[0], 0);
+        wait(&sm.done[0], 0);
       }
       __syncwarp();
     } else if (warp == 2) {
@@ -318,21 +301,21 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
 #pragma unroll 1
           for (int u = 0; u < units; ++u, ++n) {
             const uint32_t t = n & 1, b = n & 3, sv = pages % kBStages;
-            if (!wait(&sm.p_full[b], (n / 4) & 1) || !wait(&sm.vb_full[sv], (pages / kBStages) & 1)) break;
+            wait(&sm.vb_full[sv], (pages / kBStages) & 1);
+            wait(&sm.p_full[b], (n / 4) & 1);
             tc_fence_after();
-            const uint32_t v = v0 + (sv * (kPage * 2)) / 16;
+            const uint32_t v = v0 + sv * (kPage * 2 / 16);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
               tc_mma_ts_lo(tmem + kColO + t * 128, tmem + kColS + b * 64 + kk * 8, v + kk * 128, hi, id, u >= 2 || kk > 0);
             tc_commit(&sm.pv_done[b]);
-            if (same || t == 1) {
-              tc_commit(&sm.vb_empty[sv]);
-              ++pages;
-            }
+            const bool last = same || t == 1;
+            tc_commit_if(&sm.vb_empty[sv], last);
+            pages += last;
           }
         }
         tc_commit(&sm.done[1]);
-        ok &= mbar_wait_short(&sm.done[1], 0);
+        wait(&sm.done[1], 0);
       }
       __syncwarp();
     }
@@ -401,47 +384,35 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         ++items;
       }
       const int pages = (walk.g.s1 - walk.g.s0) * (shared_rows(it) ? 2 : 1);
-      constexpr int C = D / 16, R = 128 / C;  // 16 dims of a row, rows at a time
+      constexpr int C = D / 8, R = 128 / C;  // 8 dims of a row, rows at a time
       const int r0 = c / C, e = c % C;
+      // (row & 7 and the bits of the swizzle are the same for all of a thread's rows, R apart)
+      const int from = swizzled<D>(r0, e * 8), to = (e / 8) * (kBlock * 128) + r0 * 128 + (((e & 7) ^ (r0 & 7)) << 4);
 #pragma unroll 1
       for (int s = 0; s < pages; ++s, ++n) {
         const uint32_t sv = n % kVStages, b = n % kBStages;
         warp_wait(&sm.vc_full[sv], (n / kVStages) & 1);
-        uint4 in[kBlock / R];
+        uint2 in[kBlock / R];
 #pragma unroll
-        for (int i = 0; i < kBlock / R; ++i) in[i] = *reinterpret_cast<const uint4*>(sm.vc[sv] + swizzled<D>(i * R + r0, e * 16));
+        for (int i = 0; i < kBlock / R; ++i) in[i] = *reinterpret_cast<const uint2*>(sm.vc[sv] + from + i * R * D);
         const float vs = sm.meta[n % kMetas].vs;
         // 2^120 vs, in one factor where it fits
         const bool two = vs > 64.f;
         const float f1 = two ? 0x1p120f : vs * 0x1p60f * 0x1p60f;
         const uint32_t m1 = pack_bf16(f1, f1), m2 = pack_bf16(vs, vs);
         warp_wait(&sm.vb_empty[b], ((n / kBStages) & 1) ^ 1);
-        uint8_t* to = sm.vb[b] + (e / 4) * (kBlock * 128);
 #pragma unroll
         for (int i = 0; i < kBlock / R; ++i) {
-          const int row = i * R + r0;
-          uint4 out[2];
-          codes_to_bf16(in[i].x, m1, &out[0].x, &out[0].y);
-          codes_to_bf16(in[i].y, m1, &out[0].z, &out[0].w);
-          codes_to_bf16(in[i].z, m1, &out[1].x, &out[1].y);
-          codes_to_bf16(in[i].w, m1, &out[1].z, &out[1].w);
-          if (__builtin_expect(two, 0)) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              out[j] = make_uint4(mul_bf16x2(out[j].x, m2), mul_bf16x2(out[j].y, m2), mul_bf16x2(out[j].z, m2), mul_bf16x2(out[j].w, m2));
-          }
-          // (lanes of the upper slab store their second half first: no two of eight lanes meet in a bank)
-          const bool flip = (e & 4) != 0;
-          const int c0 = (e & 3) * 2;
-          *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 1 : 0)) ^ (row & 7)) << 4)) = flip ? out[1] : out[0];
-          *reinterpret_cast<uint4*>(to + row * 128 + (((c0 + (flip ? 0 : 1)) ^ (row & 7)) << 4)) = flip ? out[0] : out[1];
+          uint4 out;
+          codes_to_bf16(in[i].x, m1, &out.x, &out.y);
+          codes_to_bf16(in[i].y, m1, &out.z, &out.w);
+          if (__builtin_expect(two, 0)) out = make_uint4(mul_bf16x2(out.x, m2), mul_bf16x2(out.y, m2), mul_bf16x2(out.z, m2), mul_bf16x2(out.w, m2));
+          *reinterpret_cast<uint4*>(sm.vb[b] + to + i * R * 128) = out;
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&sm.vb_full[b]);
-          mbar_arrive(&sm.vc_empty[sv]);
-        }
+        mbar_arrive_if(&sm.vb_full[b], lane == 0);
+        mbar_arrive_if(&sm.vc_empty[sv], lane == 0);
       }
     }
   } else {
@@ -452,7 +423,6 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t col_o = tmem + lanes + kColO + t * 128;
     uint32_t items = 0, n = 0, kn = 0, merges = 0;  // items, units of this tile, pages before the item's first
-    Kv8Segment cut0, cut1;  // of the items that the run shares with others: its first and its last
     int n_cut = 0;
     while (walk.next(a, w, sm.plan)) {
       const Kv8Item& it = walk.g.it;
@@ -467,43 +437,44 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         __syncwarp();
         if (lane == 0) mbar_arrive(&sm.q_free);
       }
-      float ref = kNone;
-      uint64_t sum[2] = {0, 0};
+      float ref = kNone, l = 0.f;
 #pragma unroll 1
       for (int u = 0; u < units; ++u, ++n) {
         const uint32_t b = (n & 1) * 2 + t, col_s = tmem + lanes + kColS + b * 64;
         wait(&sm.s_full[b], (n / 2) & 1);
         __syncwarp();
         tc_fence_after();
-        uint32_t x[64];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) tmem_ld32(col_s + i * 32, *reinterpret_cast<uint32_t(*)[32]>(x + i * 32));
+        uint32_t x[64], p[32];
+        const auto load = [&]() {
+          tmem_ld32(col_s, *reinterpret_cast<uint32_t(*)[32]>(x));
+          tmem_ld32(col_s + 32, *reinterpret_cast<uint32_t(*)[32]>(x + 32));
+        };
+        load();
         const PageMeta meta = sm.meta[(kn + (same ? 2 * u + t : u)) % kMetas];
         const float c = fmaxf(qs * meta.ks, 0x1p-126f);  // (never 0: scores may be -inf)
         const bool masked = meta.pos < 0 || meta.pos + kBlock > lim_low;
         tc_wait_ld();
-        if (__builtin_expect(masked, 0)) {
+        const auto mask = [&]() {
           const int lim0 = meta.pos < 0 ? 0 : lim - meta.pos;
 #pragma unroll
           for (int i = 0; i < 64; ++i)
             if (i >= lim0) x[i] = 0xff800000u;
-        }
-        float top;
-        {
-          float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        };
+        if (__builtin_expect(masked, 0)) mask();
+        float more = weights(x, c, -ref, p);
+        // The weights' sum tells whether the reference is still good (at an item's begin it is not: the sum is infinite).  The maximum
+        // of the scores is looked for only where it is not.
+        if (__builtin_expect(__any_sync(0xffffffffu, more > kMost), 0)) {
+          load();
+          tc_wait_ld();
+          if (masked) mask();
+          float top = -INFINITY;
 #pragma unroll
-          for (int i = 0; i < 64; i += 8) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) m[j] = max3(m[j], __uint_as_float(x[i + 2 * j]), __uint_as_float(x[i + 2 * j + 1]));
-          }
-          top = max3(fmaxf(m[0], m[1]), m[2], m[3]) * c;
-        }
-        if (__builtin_expect(__any_sync(0xffffffffu, top > ref + kGrow), 0)) {
-          const float to = top > ref + kGrow ? top : ref, f = ex2(ref - to);
+          for (int i = 0; i < 64; i += 2) top = max3(top, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+          top *= c;
+          const float to = more > kMost && top > ref ? top : ref, f = ex2(ref - to);
           ref = to;
-          const uint64_t f2 = pair(f, f);
-          sum[0] = fma2(sum[0], f2, 0);
-          sum[1] = fma2(sum[1], f2, 0);
+          l *= f;
           if (u > 0) {
             wait(&sm.pv_done[((n - 1) & 1) * 2 + t], ((n - 1) / 2) & 1);  // (those before have been, or these scores were not there)
             __syncwarp();
@@ -518,19 +489,16 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
               tmem_st16(col_o + i, o);
             }
           }
+          more = weights(x, c, -ref, p);
         }
-        uint32_t p[32];
-        weights<kPoly>(x, c, -ref, sum, p);
-        weights<kPoly>(x + 32, c, -ref, sum, p + 16);
         tmem_st32(col_s, p);
+        l += more;
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.p_full[b]);
+        mbar_arrive_if(&sm.p_full[b], lane == 0);
       }
       kn += units * (same ? 2 : 1);
-      const float2 s0 = unpair(sum[0]), s1 = unpair(sum[1]);
-      float l = (s0.x + s0.y) + (s1.x + s1.y);
       wait(&sm.pv_done[((n - 1) & 1) * 2 + t], ((n - 1) / 2) & 1);
       __syncwarp();
       tc_fence_after();
@@ -607,15 +575,15 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       __syncwarp();
       if (same && lane == 0) mbar_arrive(&sm.q_free);
       if (!whole) {
-        if (n_cut++ == 0) cut0 = walk.g;
-        else cut1 = walk.g;
+        if (r == 0) sm.cut[t][n_cut & 1] = walk.g;
+        ++n_cut;
       }
     }
     // ---- items that other CTAs have parts of: the last one to get here joins them
 #pragma unroll 1
     for (int i = 0; i < n_cut; ++i) {
-      const Kv8Segment g = i == 0 ? cut0 : cut1;
       tile_sync(t);
+      const Kv8Segment& g = sm.cut[t][i];
       if (r == 0) {
         bool last = false;
         if (ok) {  // (what the tile has written before the barrier goes before, what it reads behind it comes after)

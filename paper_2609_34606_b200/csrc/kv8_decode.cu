@@ -203,10 +203,11 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
   Kv8Walk walk;
+  uint32_t tries = 0;
   bool ok = true;  // false: a wait ran out; nothing more is waited for
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok) ok = mbar_wait_short(bar, parity);
-    return ok;
+    tries = mbar_poll(bar, parity, tries);
+    return ok = tries == 0;
   };
   // the same for a whole warp that stays together
   const auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
@@ -261,8 +262,8 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
     }
     if (!ok)  // pages that nobody took: their loads must not outlive the CTA
       for (uint32_t i = 1; i <= kStages && i <= n; ++i) {
-        mbar_wait_short(&sm.k_full[(n - i) % kStages], ((n - i) / kStages) & 1);
-        mbar_wait_short(&sm.v_full[(n - i) % kStages], ((n - i) / kStages) & 1);
+        mbar_poll(&sm.k_full[(n - i) % kStages], ((n - i) / kStages) & 1, 0);
+        mbar_poll(&sm.v_full[(n - i) % kStages], ((n - i) / kStages) & 1, 0);
       }
   } else if (warp == 1) {
     // ---- first products
@@ -291,7 +292,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         ++items;
       }
       tc_commit(&sm.done[0]);
-      mbar_wait_short(&sm.done[0], 0);
+      mbar_poll(&sm.done[0], 0, 0);
     }
     __syncwarp();
   } else if (warp == 3) {
@@ -325,7 +326,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         }
       }
       tc_commit(&sm.done[1]);
-      mbar_wait_short(&sm.done[1], 0);
+      mbar_poll(&sm.done[1], 0, 0);
     }
     __syncwarp();
   } else if (warp == 2) {

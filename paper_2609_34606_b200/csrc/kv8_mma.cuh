@@ -21,27 +21,37 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 // mbar_wait in a handful of instructions: the roles of these kernels share the instruction caches of their SM, and the
-// unrolled loop, at every wait, costs more than the waits do.
-__device__ __forceinline__ bool mbar_wait_short(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
+// unrolled loop, at every wait, costs more than the waits do.  `tries` is how many polls have been spent without success: 0, or,
+// after a wait that ran out, kMaxPolls, with which this one and all later ones give up at once.  Returns the new one.
+// (a poll may sleep for some 20 us: without that the waiting warps' polls take issue slots from the others)
+constexpr uint32_t kMaxPolls = 1u << 17;
+__device__ __forceinline__ uint32_t mbar_poll(uint64_t* bar, uint32_t parity, uint32_t tries) {
+  uint32_t after;
   asm volatile(
       "{\n"
       ".reg .pred p, q;\n"
       ".reg .u32 n;\n"
-      "mov.u32 n, 0;\n"
+      "mov.u32 n, %3;\n"
       "AGAIN:\n"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n"
       "@p bra DONE;\n"
       "add.u32 n, n, 1;\n"
-      "setp.lt.u32 q, n, 4194304;\n"
+      "setp.lt.u32 q, n, %4;\n"
       "@q bra AGAIN;\n"
       "DONE:\n"
-      "selp.u32 %0, 1, 0, p;\n"
+      "selp.u32 %0, %3, %4, p;\n"
       "}\n"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
+      : "=r"(after)
+      : "r"(smem_u32(bar)), "r"(parity), "r"(tries), "n"(kMaxPolls)
       : "memory");
-  return ok;
+  return after;
+}
+// arrivals and commits by some threads or sometimes, without a branch
+__device__ __forceinline__ void mbar_arrive_if(uint64_t* bar, bool yes) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(smem_u32(bar)), "r"(static_cast<uint32_t>(yes)) : "memory");
+}
+__device__ __forceinline__ void tc_commit_if(uint64_t* bar, bool yes) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar)), "r"(static_cast<uint32_t>(yes)) : "memory");
 }
 // the bytes alone: the arrival comes later
 __device__ __forceinline__ void mbar_expect_tx_only(uint64_t* bar, uint32_t bytes) {
@@ -67,6 +77,25 @@ __device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo) {
   return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(lbo >> 4) << 16 |
          static_cast<uint64_t>((8 * D) >> 4) << 32 | static_cast<uint64_t>(1) << 46 |
          static_cast<uint64_t>(D == 128 ? 2 : 4) << 61;
+}
+// The two words of it, without a leading offset.
+__device__ __forceinline__ uint32_t row_desc_lo(uint32_t addr) { return (addr & 0x3FFFFu) >> 4; }
+template <int D>
+__host__ __device__ constexpr uint32_t row_desc_hi() {
+  return ((8 * D) >> 4) | 1u << 14 | (D == 128 ? 2u : 4u) << 29;
+}
+__device__ __forceinline__ void mma_f8_lo(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      ".reg .b64 da, db;\n"
+      "setp.ne.b32 p, %5, 0;\n"
+      "mov.b64 da, {%1, %3};\n"
+      "mov.b64 db, {%2, %3};\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n"
+      "}\n" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      : "memory");
 }
 // Byte of (row, byte in the row) in such a tile.
 template <int D>
