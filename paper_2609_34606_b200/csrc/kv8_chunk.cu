@@ -4,22 +4,26 @@
 // fit beside them: an exponential for every pair (16 a clock on an SM, which is what the products of D = 128 take as well)
 // and the values' way from 8 bits to 16.
 //   S [128 rows x 64 keys] = (Qhi + Qlo) [128 x D] K^T [D x 64]   e4m3 codes as TMA leaves them; the queries in two terms,
-//                                                                  which together take as long as one product of bf16
-//   O [128 rows x D]      += P [128 x 64 keys] V [64 x D]          bf16: P from tensor memory, V from shared memory
+//                                                                  which together take as long as one product of 16 bits
+//   O [128 rows x D]      += P [128 x 64 keys] V [64 x D]          fp16: P from tensor memory, V from shared memory
 // A query is hi = e4m3(x), lo = e4m3(x - hi), x scaled by a power of two that brings its row's largest value to 2^7 .. 2^8:
-// bf16 values stay exact unless they are below 2^-10 of that, which may lose 2^-18 of it.  The keys' scales are left to the
-// softmax, where they are part of the factor that scores are multiplied by anyhow.  The values become bf16 with their scale in
-// them, which is exact: a code has 4 significant bits, and bf16 has the range of fp32.  So weights need no more than bf16
-// either, whatever the scales of other pages are.
+// bf16 values stay exact unless they are below 2^-10 of that, which may lose 2^-18 of it.  The codes of the values become fp16,
+// which is exact.  Scales are left to the softmax: a page's key scale is in the factor that scores are multiplied by anyhow, its
+// value scale in what is added in the exponent (and taken out of the sum of weights again).  So P holds weight times value scale.
+// It is set up to have its largest value at 2^8 and may grow to 2^15; what fp16 cannot hold beside that, below 2^-25, is less than
+// 2^-33 of the largest contribution.
 //
-// An item has 256 rows, two tiles of 128, so that every page that is read and turned into bf16 serves both.  A tile's S has
+// An item has 256 rows, two tiles of 128, so that every page that is read and turned into fp16 serves both.  A tile's S has
 // two buffers of a page's 64 keys: the products of a page run while the softmax is at the page before it.  (With one buffer of
-// 128 keys, products and softmax of a tile wait for each other: 1800 us instead of 1319 for 4680 x 46,800 x 12 heads.)  An item of 128
-// rows or fewer gives both tiles to the same rows: they take its pages in turn and are brought together at its end.
+// 128 keys products are a fifth faster, but products and softmax of a tile wait for each other: 1543 us instead of XXX for 4680
+// queries, 46,800 tokens, 12 heads.)  An item of 128 rows or fewer gives both tiles to the same rows: they take its pages in
+// turn and are brought together at its end.
 //
-// Warps: 0 loads pages, 1 issues the scores' products, 2 those of the values, 4 - 7 turn values into bf16 and, an item ahead, queries into their two terms, 8 - 11
-// and 12 - 15 are the softmax of a tile each, a row to a thread.
-// Tensor memory: four S (P, packed bf16, over their first halves), O of both tiles.
+// Warps: 0 loads pages, 1 and 2 issue the products of a tile each, 4 - 7 turn values into fp16 and, an item ahead, queries into
+// their two terms, 8 - 11 and 12 - 15 are the softmax of a tile each, a row to a thread.
+// The warps that issue products stay together and choose a lane for it at the last moment: so their operands are in uniform
+// registers.  A loop of one lane alone takes some 75 cycles to issue a product, beside busy warps, more than the product's 64.
+// Tensor memory: four S (P, packed fp16, over their first halves), O of both tiles.
 #include "kv8.cuh"
 #include "kv8_mma.cuh"
 
@@ -29,7 +33,8 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kTile = 128;          // rows of a tile
-constexpr float kMost = 8192.f;     // weights of a page's 64 keys may add up to this before a row's reference is set anew: sums and O have room for that
+constexpr float kMost = 32768.f;    // what a page's 64 keys may add up to in P before a row's reference is set anew
+constexpr float kShift = 8.f;       // ... to have the largest at 2^8
 constexpr int kMetas = 16;
 
 template <int D>
@@ -42,7 +47,7 @@ struct ChunkSmem {
   };
   uint8_t k[kKStages][kPage];
   uint8_t vc[kVStages][kPage];         // codes
-  uint8_t vb[kBStages][kPage * 2];     // bf16, [64 dims][key][64 dims], dims of a group of four in the order 0, 2, 1, 3
+  uint8_t vb[kBStages][kPage * 2];     // fp16, [64 dims][key][64 dims]
   float qscale[2 * kTile];
   float other_ref[kTile], other_sum[kTile];
   PageMeta meta[kMetas];
@@ -83,7 +88,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return m;
 }
 
-// Weights of 64 keys: 2^(s * c + nref) as bf16 pairs, and their sum in fp32.  The order of the instructions is made by hand: a
+// Weights of 64 keys: 2^(s * c + nref) as fp16 pairs, and their sum in fp32.  The order of the instructions is made by hand: a
 // pair's exponentials come kLag pairs behind its product, its sum and rounding another kLag behind them, so that nothing waits
 // for its operands (the compiler's order leaves a lone warp waiting at each of them).
 constexpr int kLag = 4;
@@ -98,38 +103,22 @@ __device__ __forceinline__ float weights(uint32_t* s, float c, float nref, uint3
     if (j >= 0 && j < 32) asm volatile("ex2.approx.ftz.f32 %0, %0;\nex2.approx.ftz.f32 %1, %1;\n" : "+r"(s[2 * j]), "+r"(s[2 * j + 1]));
     const int k = i - 2 * kLag;
     if (k >= 0)
-      asm volatile("{\n.reg .b64 t;\nmov.b64 t, {%2, %3};\nadd.rn.f32x2 %0, %0, t;\ncvt.rn.bf16x2.f32 %1, %3, %2;\n}\n" : "+l"(sum[k & 1]), "=r"(w[k]) : "r"(s[2 * k]), "r"(s[2 * k + 1]));
+      asm volatile("{\n.reg .b64 t;\nmov.b64 t, {%2, %3};\nadd.rn.f32x2 %0, %0, t;\ncvt.rn.f16x2.f32 %1, %3, %2;\n}\n" : "+l"(sum[k & 1]), "=r"(w[k]) : "r"(s[2 * k]), "r"(s[2 * k + 1]));
   }
   const float2 a = unpair(sum[0]), b = unpair(sum[1]);
   return (a.x + a.y) + (b.x + b.y);
 }
 
-// Four e4m3 codes as bf16: (0, 2) and (1, 3).  A code's bits, put where bf16 has them, are the value times 2^-120, subnormal
-// ones too, and there is no code that gives Inf or NaN; the rest is a product by a power of two, or by two of them (m1, m2) where one would pass the range.
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+// two e4m3 codes as fp16
+__device__ __forceinline__ uint32_t fp16_of(uint32_t two) {
   uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\ncvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(d) : "r"(two));
   return d;
 }
-__device__ __forceinline__ void codes_to_bf16(uint32_t w, uint32_t m1, uint32_t* even, uint32_t* odd) {
-  *even = mul_bf16x2(((w << 8) & 0x80008000u) | ((w << 4) & 0x07f007f0u), m1);
-  *odd = mul_bf16x2((w & 0x80008000u) | ((w >> 4) & 0x07f007f0u), m1);
-}
-
 __device__ __forceinline__ uint32_t e4m3x2(float a, float b) { return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3); }
 __device__ __forceinline__ float2 from_e4m3x2(uint32_t two) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
-
-// D dims of the output's row: columns of four come as 0, 2, 1, 3.
-__device__ __forceinline__ void to_order(uint32_t* o) {
-#pragma unroll
-  for (int i = 0; i < 32; i += 4) {
-    const uint32_t t = o[i + 1];
-    o[i + 1] = o[i + 2];
-    o[i + 2] = t;
-  }
 }
 
 __device__ __forceinline__ void tile_sync(int tile) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + tile) : "memory"); }
@@ -151,7 +140,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
   if (tid == 0) {
     for (int i = 0; i < kKStages; ++i) {
       mbar_init(&sm.k_full[i], 1);
-      mbar_init(&sm.k_empty[i], 1);
+      mbar_init(&sm.k_empty[i], 2);
     }
     for (int i = 0; i < kVStages; ++i) {
       mbar_init(&sm.vc_full[i], 1);
@@ -159,7 +148,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     }
     for (int i = 0; i < kBStages; ++i) {
       mbar_init(&sm.vb_full[i], 4);
-      mbar_init(&sm.vb_empty[i], 1);
+      mbar_init(&sm.vb_empty[i], 2);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&sm.s_full[i], 1);
@@ -167,7 +156,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       mbar_init(&sm.pv_done[i], 1);
     }
     mbar_init(&sm.q_full, 4);
-    mbar_init(&sm.q_free, 1 + 8);  // its products, and the softmax warps (scales; the merge of two tiles)
+    mbar_init(&sm.q_free, 2 + 8);  // its products, and the softmax warps (scales; the merge of two tiles)
     mbar_init(&sm.other_full, 4);
     mbar_init(&sm.done[0], 1);
     mbar_init(&sm.done[1], 1);
@@ -210,13 +199,13 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         const int per = shared_rows(it) ? 2 : 1, s1 = walk.g.s1 * per;  // pages
         for (int s = walk.g.s0 * per; s < s1 && ok; s += 32) {
           int blk = 0, page = -1;
-          PageMeta meta{-1, 1.f, 0.f};
+          PageMeta meta{-1, 1.f, 1.f};
           if (s + lane < s1) page = kv8_page(a, it, s + lane, &blk);
           if (page >= 0) {
             const int64_t ph = static_cast<int64_t>(page) * a.Hkv + it.h;
             meta.pos = blk * kBlock;
             meta.ks = __ldg(a.k_scale + ph);
-            meta.vs = __ldg(a.v_scale + ph);
+            meta.vs = fmaxf(__ldg(a.v_scale + ph), 0x1p-60f);  // (0 is no scale; it would leave NaN)
           }
           const int count = min(32, s1 - s);
 #pragma unroll 1
@@ -254,70 +243,85 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         for (uint32_t i = 1; i <= kKStages && i <= n; ++i) mbar_poll(&sm.k_full[(n - i) % kKStages], ((n - i) / kKStages) & 1, 0);
         for (uint32_t i = 1; i <= kVStages && i <= n; ++i) mbar_poll(&sm.vc_full[(n - i) % kVStages], ((n - i) / kVStages) & 1, 0);
       }
-    } else if (warp == 1) {
-      // ---- scores.  Unit u of an item: tile u % 2 and a page; units are counted through, and have the buffers of S in turn.
-      if (elect_one_sync()) {
-        constexpr uint32_t id = idesc_e4m3(128, kBlock, 0, 0);
-        const uint32_t q0 = row_desc_lo(smem_u32(sm.q)), k0 = row_desc_lo(smem_u32(sm.k));
-        uint32_t items = 0, n = 0, st = 0, round = 0;
-        while (ok && walk.next(a, w, sm.plan)) {
-          const bool same = shared_rows(walk.g.it);
-          const int units = 2 * (walk.g.s1 - walk.g.s0);
-          if (!wait(&sm.q_full, items++ & 1)) break;
-#pragma unroll 1
-          for (int u = 0; u < units; ++u, ++n) {
-            const uint32_t t = n & 1, b = n & 3;
-            wait(&sm.k_full[st], round & 1);
-            wait(&sm.pv_done[b], ((n / 4) & 1) ^ 1);
-            tc_fence_after();
-            const uint32_t q = q0 + (same ? 0 : t) * (2 * kTile * D / 16), k = k0 + st * (kPage / 16);
+    } else if (warp <= 2) {
+      // ---- products of a tile.  A unit is a page of the item (of shared rows: every other page); scores are two units ahead, and
+      // go over the weights of a page as soon as those have been issued: the products run in the order of their issue.
+      constexpr uint32_t id_s = idesc_e4m3(128, kBlock, 0, 0), id_o = idesc_fp16(128, D, 0, 1), hi_v = desc_hi_sw128(1024);
+      const uint32_t t = warp_uniform(warp - 1), tm = warp_uniform(tmem);
+      const uint32_t q0 = row_desc_lo(smem_u32(sm.q)), k0 = row_desc_lo(smem_u32(sm.k)), v0 = desc_lo_sw128(smem_u32(sm.vb), kBlock * 128);
+      const uint32_t s0 = tm + kColS + t * 64, o0 = tm + kColO + t * 128;
+      uint32_t items = 0, ns = 0, n = 0, st = 0, round = 0, nv = 0;  // items; units of scores, of values; stages of K and V
+      const auto next_stage = [&]() {
+        ++st;
+        round += st == kKStages;
+        st = st == kKStages ? 0 : st;
+      };
+      // the other tile's page
+      const auto pass_keys = [&]() {
+        wait(&sm.k_full[st], round & 1);
+        mbar_arrive_if(&sm.k_empty[st], lane == 0);
+        next_stage();
+      };
+      const auto pass_values = [&]() {
+        wait(&sm.vb_full[nv % kBStages], (nv / kBStages) & 1);
+        mbar_arrive_if(&sm.vb_empty[nv % kBStages], lane == 0);
+        ++nv;
+      };
+      while (warp_uniform(walk.next(a, w, sm.plan))) {
+        const uint32_t same = warp_uniform(shared_rows(walk.g.it)), units = warp_uniform(walk.g.s1 - walk.g.s0);
+        const uint32_t q = q0 + (same ? 0 : t) * (2 * kTile * D / 16);
+        const auto scores = [&](uint32_t u) {
+          tc_fence_after();
+          const uint32_t k = k0 + st * (kPage / 16), d = s0 + (ns & 1) * 128, b = (ns & 1) * 2 + t;
+          if (elect_one_sync()) {
 #pragma unroll
             for (int term = 0; term < 2; ++term)
 #pragma unroll
               for (int kk = 0; kk < D / 32; ++kk)
-                mma_f8_lo(tmem + kColS + b * 64, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, row_desc_hi<D>(), id, term + kk > 0);
+                mma_f8_lo(d, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, row_desc_hi<D>(), id_s, term + kk > 0);
             tc_commit(&sm.s_full[b]);
-            const bool last = same || t == 1;  // of the page
-            tc_commit_if(&sm.k_empty[st], last);
-            st += last;
-            round += st == kKStages;
-            st = st == kKStages ? 0 : st;
+            tc_commit(&sm.k_empty[st]);
+            if (u + 1 == units) tc_commit(&sm.q_free);
           }
-          tc_commit(&sm.q_free);
+          __syncwarp();
+          next_stage();
+          ++ns;
+          if (same && !(t && u + 1 == units)) pass_keys();
+        };
+        wait(&sm.q_full, items & 1);
+        ++items;
+        if (same && t) {
+          pass_keys();
+          pass_values();
         }
-        tc_commit(&sm.done[0]);
-        wait(&sm.done[0], 0);
-      }
-      __syncwarp();
-    } else if (warp == 2) {
-      // ---- values
-      if (elect_one_sync()) {
-        constexpr uint32_t id = idesc_bf16_f32(128, D, 0, 1), hi = desc_hi_sw128(1024);
-        const uint32_t v0 = desc_lo_sw128(smem_u32(sm.vb), kBlock * 128);
-        uint32_t n = 0, pages = 0;
-        while (ok && walk.next(a, w, sm.plan)) {
-          const bool same = shared_rows(walk.g.it);
-          const int units = 2 * (walk.g.s1 - walk.g.s0);
+        for (uint32_t u = 0; u < 2 && u < units; ++u) {
+          wait(&sm.k_full[st], round & 1);
+          scores(u);
+        }
 #pragma unroll 1
-          for (int u = 0; u < units; ++u, ++n) {
-            const uint32_t t = n & 1, b = n & 3, sv = pages % kBStages;
-            wait(&sm.vb_full[sv], (pages / kBStages) & 1);
-            wait(&sm.p_full[b], (n / 4) & 1);
-            tc_fence_after();
-            const uint32_t v = v0 + sv * (kPage * 2 / 16);
+        for (uint32_t u = 0; u < units; ++u, ++n) {
+          // (what the next scores need is waited for before the weights are: they follow those at once)
+          const bool ahead = u + 2 < units;
+          if (ahead) wait(&sm.k_full[st], round & 1);
+          const uint32_t sv = nv % kBStages, v = v0 + sv * (kPage * 2 / 16), b = (n & 1) * 2 + t, pw = s0 + (n & 1) * 128;
+          wait(&sm.vb_full[sv], (nv / kBStages) & 1);
+          wait(&sm.p_full[b], (n / 2) & 1);
+          tc_fence_after();
+          if (elect_one_sync()) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              tc_mma_ts_lo(tmem + kColO + t * 128, tmem + kColS + b * 64 + kk * 8, v + kk * 128, hi, id, u >= 2 || kk > 0);
+            for (int kk = 0; kk < 4; ++kk) tc_mma_ts_lo(o0, pw + kk * 8, v + kk * 128, hi_v, id_o, u > 0 || kk > 0);
             tc_commit(&sm.pv_done[b]);
-            const bool last = same || t == 1;
-            tc_commit_if(&sm.vb_empty[sv], last);
-            pages += last;
+            tc_commit(&sm.vb_empty[sv]);
           }
+          __syncwarp();
+          ++nv;
+          if (ahead) scores(u + 2);
+          if (same && !(t && u + 1 == units)) pass_values();
         }
-        tc_commit(&sm.done[1]);
-        wait(&sm.done[1], 0);
       }
+      if (elect_one_sync()) tc_commit(&sm.done[t]);
       __syncwarp();
+      wait(&sm.done[t], 0);
     }
   } else if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
@@ -392,22 +396,16 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       for (int s = 0; s < pages; ++s, ++n) {
         const uint32_t sv = n % kVStages, b = n % kBStages;
         warp_wait(&sm.vc_full[sv], (n / kVStages) & 1);
+        const bool there = sm.meta[n % kMetas].pos >= 0;  // (else: zeros, which is what weights of 0 can bear)
         uint2 in[kBlock / R];
 #pragma unroll
         for (int i = 0; i < kBlock / R; ++i) in[i] = *reinterpret_cast<const uint2*>(sm.vc[sv] + from + i * R * D);
-        const float vs = sm.meta[n % kMetas].vs;
-        // 2^120 vs, in one factor where it fits
-        const bool two = vs > 64.f;
-        const float f1 = two ? 0x1p120f : vs * 0x1p60f * 0x1p60f;
-        const uint32_t m1 = pack_bf16(f1, f1), m2 = pack_bf16(vs, vs);
         warp_wait(&sm.vb_empty[b], ((n / kBStages) & 1) ^ 1);
 #pragma unroll
         for (int i = 0; i < kBlock / R; ++i) {
-          uint4 out;
-          codes_to_bf16(in[i].x, m1, &out.x, &out.y);
-          codes_to_bf16(in[i].y, m1, &out.z, &out.w);
-          if (__builtin_expect(two, 0)) out = make_uint4(mul_bf16x2(out.x, m2), mul_bf16x2(out.y, m2), mul_bf16x2(out.z, m2), mul_bf16x2(out.w, m2));
-          *reinterpret_cast<uint4*>(sm.vb[b] + to + i * R * 128) = out;
+          if (!there) in[i] = make_uint2(0, 0);
+          *reinterpret_cast<uint4*>(sm.vb[b] + to + i * R * 128) =
+              make_uint4(fp16_of(in[i].x), fp16_of(in[i].x >> 16), fp16_of(in[i].y), fp16_of(in[i].y >> 16));
         }
         fence_proxy_async_smem();
         __syncwarp();
@@ -452,18 +450,19 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         load();
         const PageMeta meta = sm.meta[(kn + (same ? 2 * u + t : u)) % kMetas];
         const float c = fmaxf(qs * meta.ks, 0x1p-126f);  // (never 0: scores may be -inf)
+        const float lv = static_cast<float>(static_cast<int>(__float_as_uint(meta.vs) >> 23) - 127);
         const bool masked = meta.pos < 0 || meta.pos + kBlock > lim_low;
-        tc_wait_ld();
         const auto mask = [&]() {
           const int lim0 = meta.pos < 0 ? 0 : lim - meta.pos;
 #pragma unroll
           for (int i = 0; i < 64; ++i)
             if (i >= lim0) x[i] = 0xff800000u;
         };
+        tc_wait_ld();
         if (__builtin_expect(masked, 0)) mask();
-        float more = weights(x, c, -ref, p);
-        // The weights' sum tells whether the reference is still good (at an item's begin it is not: the sum is infinite).  The maximum
-        // of the scores is looked for only where it is not.
+        float more = weights(x, c, lv - ref, p);
+        // The sum tells whether the reference is still good (at an item's begin it is not: the sum is infinite).  The maximum of the
+        // scores is looked for only where it is not.
         if (__builtin_expect(__any_sync(0xffffffffu, more > kMost), 0)) {
           load();
           tc_wait_ld();
@@ -471,7 +470,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           float top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 64; i += 2) top = max3(top, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-          top *= c;
+          top = top * c + (lv - kShift);
           const float to = more > kMost && top > ref ? top : ref, f = ex2(ref - to);
           ref = to;
           l *= f;
@@ -489,10 +488,11 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
               tmem_st16(col_o + i, o);
             }
           }
-          more = weights(x, c, -ref, p);
+          // (rows whose reference stays get the weights they had)
+          more = weights(x, c, lv - ref, p);
         }
         tmem_st32(col_s, p);
-        l += more;
+        l = fmaf(more, __uint_as_float((254u << 23) - (__float_as_uint(meta.vs) & 0x7f800000u)), l);  // 1 / vs
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -546,7 +546,6 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
 #pragma unroll
           for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(sm.other[i + j][r], take, __uint_as_float(o[j]) * down));
         }
-        to_order(o);
         if (real && whole) {
 #pragma unroll
           for (int j = 0; j < 32; j += 8) {

@@ -71,6 +71,10 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, 
 __host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N, uint32_t a_mn, uint32_t b_mn) {
   return (1u << 4) | (a_mn << 15) | (b_mn << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
+// kind::f16, fp16 operands (format 0)
+__host__ __device__ constexpr uint32_t idesc_fp16(uint32_t M, uint32_t N, uint32_t a_mn, uint32_t b_mn) { return idesc_e4m3(M, N, a_mn, b_mn); }
+// lane 0's value; what comes of it is the same for the whole warp, which the compiler knows
+__device__ __forceinline__ uint32_t warp_uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 // Rows of D bytes in the swizzle that spans a row (128 bytes: layout 2, 64 bytes: layout 4); eight rows are 8 * D bytes.
 template <int D>
 __device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo) {
