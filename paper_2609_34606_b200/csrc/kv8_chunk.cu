@@ -19,7 +19,7 @@
 // queries, 46,800 tokens, 12 heads.)  An item of 128 rows or fewer gives both tiles to the same rows: they take its pages in
 // turn and are brought together at its end.
 //
-// Warps: 0 loads pages, 1 and 2 issue the products of a tile each, 4 - 7 turn values into fp16 and, an item ahead, queries into
+// Warps: 0 loads pages, 1 and 2 issue the products of a tile each, 3 looks ahead for them, 4 - 7 turn values into fp16 and, an item ahead, queries into
 // their two terms, 8 - 11 and 12 - 15 are the softmax of a tile each, a row to a thread.
 // The warps that issue products stay together and choose a lane for it at the last moment: so their operands are in uniform
 // registers.  A loop of one lane alone takes some 75 cycles to issue a product, beside busy warps, more than the product's 64.
@@ -152,7 +152,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&sm.s_full[i], 1);
-      mbar_init(&sm.p_full[i], 4);
+      mbar_init(&sm.p_full[i], 4 + 1);  // the tile's warps, and the one that looks ahead
       mbar_init(&sm.pv_done[i], 1);
     }
     mbar_init(&sm.q_full, 4);
@@ -251,27 +251,17 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       const uint32_t q0 = row_desc_lo(smem_u32(sm.q)), k0 = row_desc_lo(smem_u32(sm.k)), v0 = desc_lo_sw128(smem_u32(sm.vb), kBlock * 128);
       const uint32_t s0 = tm + kColS + t * 64, o0 = tm + kColO + t * 128;
       uint32_t items = 0, ns = 0, n = 0, st = 0, round = 0, nv = 0;  // items; units of scores, of values; stages of K and V
-      const auto next_stage = [&]() {
-        ++st;
-        round += st == kKStages;
-        st = st == kKStages ? 0 : st;
-      };
-      // the other tile's page
-      const auto pass_keys = [&]() {
-        wait(&sm.k_full[st], round & 1);
-        mbar_arrive_if(&sm.k_empty[st], lane == 0);
-        next_stage();
-      };
-      const auto pass_values = [&]() {
-        wait(&sm.vb_full[nv % kBStages], (nv / kBStages) & 1);
-        mbar_arrive_if(&sm.vb_empty[nv % kBStages], lane == 0);
-        ++nv;
-      };
       while (warp_uniform(walk.next(a, w, sm.plan))) {
         const uint32_t same = warp_uniform(shared_rows(walk.g.it)), units = warp_uniform(walk.g.s1 - walk.g.s0);
-        const uint32_t q = q0 + (same ? 0 : t) * (2 * kTile * D / 16);
-        const auto scores = [&](uint32_t u) {
-          tc_fence_after();
+        const uint32_t q = q0 + (same ? 0 : t) * (2 * kTile * D / 16), step = 1 + same, first = same & t;
+        // K's stages go round in turn
+        const auto move = [&](uint32_t by) {
+          st += by;
+          const uint32_t over = st >= kKStages;
+          round += over;
+          st -= over ? kKStages : 0;
+        };
+        const auto scores = [&](bool last) {
           const uint32_t k = k0 + st * (kPage / 16), d = s0 + (ns & 1) * 128, b = (ns & 1) * 2 + t;
           if (elect_one_sync()) {
 #pragma unroll
@@ -281,30 +271,24 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
                 mma_f8_lo(d, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, row_desc_hi<D>(), id_s, term + kk > 0);
             tc_commit(&sm.s_full[b]);
             tc_commit(&sm.k_empty[st]);
-            if (u + 1 == units) tc_commit(&sm.q_free);
+            if (last) tc_commit(&sm.q_free);
           }
           __syncwarp();
-          next_stage();
+          move(step);
           ++ns;
-          if (same && !(t && u + 1 == units)) pass_keys();
         };
         wait(&sm.q_full, items & 1);
         ++items;
-        if (same && t) {
-          pass_keys();
-          pass_values();
-        }
+        move(first);
+        nv += first;
         for (uint32_t u = 0; u < 2 && u < units; ++u) {
           wait(&sm.k_full[st], round & 1);
-          scores(u);
+          tc_fence_after();
+          scores(u + 1 == units);
         }
 #pragma unroll 1
         for (uint32_t u = 0; u < units; ++u, ++n) {
-          // (what the next scores need is waited for before the weights are: they follow those at once)
-          const bool ahead = u + 2 < units;
-          if (ahead) wait(&sm.k_full[st], round & 1);
           const uint32_t sv = nv % kBStages, v = v0 + sv * (kPage * 2 / 16), b = (n & 1) * 2 + t, pw = s0 + (n & 1) * 128;
-          wait(&sm.vb_full[sv], (nv / kBStages) & 1);
           wait(&sm.p_full[b], (n / 2) & 1);
           tc_fence_after();
           if (elect_one_sync()) {
@@ -314,14 +298,49 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
             tc_commit(&sm.vb_empty[sv]);
           }
           __syncwarp();
-          ++nv;
-          if (ahead) scores(u + 2);
-          if (same && !(t && u + 1 == units)) pass_values();
+          nv += step;
+          if (u + 2 < units) scores(u + 3 == units);
+        }
+        // (behind the item's last page)
+        nv -= first;
+        if (first) {
+          round -= st == 0;
+          st = st == 0 ? kKStages - 1 : st - 1;
         }
       }
       if (elect_one_sync()) tc_commit(&sm.done[t]);
       __syncwarp();
       wait(&sm.done[t], 0);
+    } else {
+      // ---- looks ahead for warps 1 and 2, who would otherwise poll three barriers for a page (each some 250 cycles beside busy
+      // warps): arrives with the weights of a page where its values and the keys of the scores behind it are there.  Where the
+      // tiles share rows, gives pages back for the tile that does not use them.
+      uint32_t n = 0, ks = 0, kr = 0, nv = 0;  // units of a tile before the item; stage of K, rounds; pages of V
+      const auto keys = [&](bool same) {
+        wait(&sm.k_full[ks], kr & 1);
+        mbar_arrive_if(&sm.k_empty[ks], same && lane == 0);
+        ++ks;
+        kr += ks == kKStages;
+        ks = ks == kKStages ? 0 : ks;
+      };
+      while (walk.next(a, w, sm.plan)) {
+        const bool same = shared_rows(walk.g.it);
+        const int pages = (walk.g.s1 - walk.g.s0) * (same ? 2 : 1), first = same ? 4 : 2;  // pages of the scores ahead
+        for (int m = 0; m < first && m < pages; ++m) keys(same);
+#pragma unroll 1
+        for (int m = 0; m < pages; ++m, ++nv) {
+          wait(&sm.vb_full[nv % kBStages], (nv / kBStages) & 1);
+          mbar_arrive_if(&sm.vb_empty[nv % kBStages], same && lane == 0);
+          if (m + first < pages) keys(same);
+          const uint32_t at = n + (same ? m / 2 : m), b = (at & 1) * 2;
+          for (int t = 0; t < 2; ++t) {
+            if (same && t != (m & 1)) continue;
+            if (at >= 2) wait(&sm.p_full[b + t], (at / 2 + 1) & 1);  // (the weights before these are complete)
+            mbar_arrive_if(&sm.p_full[b + t], lane == 0);
+          }
+        }
+        n += walk.g.s1 - walk.g.s0;
+      }
     }
   } else if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
