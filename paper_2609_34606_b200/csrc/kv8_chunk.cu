@@ -19,8 +19,8 @@
 // queries, 46,800 tokens, 12 heads.)  An item of 128 rows or fewer gives both tiles to the same rows: they take its pages in
 // turn and are brought together at its end.
 //
-// Warps: 0 loads pages, 1 and 2 issue the products of a tile each, 3 looks ahead for them, 4 - 7 turn values into fp16 and, an item ahead, queries into
-// their two terms, 8 - 11 and 12 - 15 are the softmax of a tile each, a row to a thread.
+// Warps: 0 loads pages, 1 and 2 issue the products of a tile each, 3 looks ahead for them, 4 - 7 turn values into fp16, 8 - 11
+// and 12 - 15 are the softmax of a tile each, a row to a thread, whose query they also bring into its two terms.
 // The warps that issue products stay together and choose a lane for it at the last moment: so their operands are in uniform
 // registers.  A loop of one lane alone takes some 75 cycles to issue a product, beside busy warps, more than the product's 64.
 // Tensor memory: four S (P, packed fp16, over their first halves), O of both tiles.
@@ -54,7 +54,7 @@ struct ChunkSmem {
   int last[2];
   Kv8Segment cut[2][2];                // [tile]: of the items that the run shares with others, its first and its last
   uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[kBStages], vb_empty[kBStages];
-  uint64_t s_full[4], p_full[4], pv_done[4], q_full, q_free, other_full, done[2];
+  uint64_t s_full[4], p_full[4], pv_done[4], q_full, other_full, done[2];
   uint32_t tmem;
   Kv8Plan plan;
 };
@@ -115,12 +115,68 @@ __device__ __forceinline__ uint32_t fp16_of(uint32_t two) {
   asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\ncvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(d) : "r"(two));
   return d;
 }
-__device__ __forceinline__ uint32_t e4m3x2(float a, float b) { return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3); }
-__device__ __forceinline__ float2 from_e4m3x2(uint32_t two) {
-  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
-  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+// A row of the queries as two e4m3 terms into row r of the tiles at q and behind it; returns what its values have been divided by.
+template <int D>
+__device__ __forceinline__ float two_terms(const __nv_bfloat16* from, bool there, uint8_t* q, int r) {
+  uint32_t x[D / 2];
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) {
+    const uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(from) + i) : make_uint4(0, 0, 0, 0);
+    x[4 * i] = v.x;
+    x[4 * i + 1] = v.y;
+    x[4 * i + 2] = v.z;
+    x[4 * i + 3] = v.w;
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < D / 2; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(x[i] & 0x7fff7fffu));
+  uint32_t top = max(m & 0xffffu, m >> 16);  // (as integers: NaN is above Inf)
+  if (__builtin_expect(top >= 0x7f80u, 0)) {
+    // what is not finite: NaN, which spoils the row and no other
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < D / 2; ++i) {
+      const uint32_t lo = x[i] & 0x7fffu, hi = x[i] >> 16 & 0x7fffu;
+      top = max(top, max(lo >= 0x7f80u ? 0 : lo, hi >= 0x7f80u ? 0 : hi));
+      x[i] |= (lo >= 0x7f80u ? 0x7fffu : 0) | (hi >= 0x7f80u ? 0x7fff0000u : 0);
+    }
+  }
+  const int ex = max(static_cast<int>(top >> 7) - 127, -100) - 7;  // (rows of zeros: any will do)
+  const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = x[4 * i + j];
+      // (fp16 has the 8 bits of these values, down to 2^-14, far below the last one of the second term)
+      asm("{\n"
+          ".reg .f32 a, b;\n"
+          ".reg .b32 y, z, lo32;\n"
+          ".reg .b16 h, l;\n"
+          "shl.b32 lo32, %2, 16;\n"
+          "mul.f32 a, lo32, %3;\n"
+          "and.b32 lo32, %2, 0xffff0000;\n"
+          "mul.f32 b, lo32, %3;\n"
+          "cvt.rn.f16x2.f32 y, b, a;\n"
+          "cvt.rn.satfinite.e4m3x2.f16x2 h, y;\n"
+          "cvt.rn.f16x2.e4m3x2 z, h;\n"
+          "sub.rn.f16x2 y, y, z;\n"
+          "cvt.rn.satfinite.e4m3x2.f16x2 l, y;\n"
+          "cvt.u32.u16 %0, h;\n"
+          "cvt.u32.u16 %1, l;\n"
+          "}\n"
+          : "=r"(hi[j]), "=r"(lo[j])
+          : "r"(w), "f"(up));
+    }
+    uint8_t* at = q + swizzled<D>(r, i * 8);
+    *reinterpret_cast<uint2*>(at) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+    *reinterpret_cast<uint2*>(at + kTile * D) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+  }
+  return __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
 }
 
+__device__ __forceinline__ void tiles_sync() { asm volatile("barrier.cta.sync 3, 256;" ::: "memory"); }
 __device__ __forceinline__ void tile_sync(int tile) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + tile) : "memory"); }
 
 // A part: a tile's O (fp32, unnormalised) as [D / 4][row][4], the rows' references and sums.
@@ -155,8 +211,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       mbar_init(&sm.p_full[i], 4 + 1);  // the tile's warps, and the one that looks ahead
       mbar_init(&sm.pv_done[i], 1);
     }
-    mbar_init(&sm.q_full, 4);
-    mbar_init(&sm.q_free, 2 + 8);  // its products, and the softmax warps (scales; the merge of two tiles)
+    mbar_init(&sm.q_full, 8);
     mbar_init(&sm.other_full, 4);
     mbar_init(&sm.done[0], 1);
     mbar_init(&sm.done[1], 1);
@@ -261,7 +316,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           round += over;
           st -= over ? kKStages : 0;
         };
-        const auto scores = [&](bool last) {
+        const auto scores = [&]() {
           const uint32_t k = k0 + st * (kPage / 16), d = s0 + (ns & 1) * 128, b = (ns & 1) * 2 + t;
           if (elect_one_sync()) {
 #pragma unroll
@@ -271,7 +326,6 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
                 mma_f8_lo(d, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, row_desc_hi<D>(), id_s, term + kk > 0);
             tc_commit(&sm.s_full[b]);
             tc_commit(&sm.k_empty[st]);
-            if (last) tc_commit(&sm.q_free);
           }
           __syncwarp();
           move(step);
@@ -284,7 +338,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         for (uint32_t u = 0; u < 2 && u < units; ++u) {
           wait(&sm.k_full[st], round & 1);
           tc_fence_after();
-          scores(u + 1 == units);
+          scores();
         }
 #pragma unroll 1
         for (uint32_t u = 0; u < units; ++u, ++n) {
@@ -299,7 +353,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           }
           __syncwarp();
           nv += step;
-          if (u + 2 < units) scores(u + 3 == units);
+          if (u + 2 < units) scores();
         }
         // (behind the item's last page)
         nv -= first;
@@ -344,69 +398,11 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     }
   } else if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    // ---- queries into two terms, values into bf16
+    // ---- values into fp16
     const int c = tid - 128;
-    uint32_t items = 0, n = 0;
+    uint32_t n = 0;
     while (walk.next(a, w, sm.plan)) {
-      const Kv8Item& it = walk.g.it;
-      {
-        constexpr int V = D / 8, R = 128 / V, kAtOnce = 4;  // vectors of a row, rows at a time, of which so many are in flight
-        const int r0 = c / V, e = c % V;
-        const int rows = shared_rows(it) ? kTile : 2 * kTile;
-        bool waited = false;
-#pragma unroll 1
-        for (int base = 0; base < rows; base += R * kAtOnce) {
-          uint4 in[kAtOnce];
-#pragma unroll
-          for (int i = 0; i < kAtOnce; ++i) {
-            const int r = base + i * R + r0;
-            in[i] = make_uint4(0, 0, 0, 0);
-            if (r < it.rows) {
-              const int at = it.row0 + r;
-              in[i] = __ldg(reinterpret_cast<const uint4*>(a.q + (it.first + at / a.group) * a.ts + (it.h * a.group + at % a.group) * a.hs + e * 8));
-            }
-          }
-          if (!waited) {
-            warp_wait(&sm.q_free, (items & 1) ^ 1);
-            waited = true;
-          }
-#pragma unroll
-          for (int i = 0; i < kAtOnce; ++i) {
-            const int r = base + i * R + r0;
-            const uint32_t words[4] = {in[i].x, in[i].y, in[i].z, in[i].w};
-            float x[8];
-            float top = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              x[j] = __uint_as_float(j & 1 ? words[j / 2] & 0xffff0000u : words[j / 2] << 16);
-              // (what is not finite: NaN, which spoils the row and no other)
-              if (fabsf(x[j]) < INFINITY) top = fmaxf(top, fabsf(x[j]));
-              else x[j] = NAN;
-            }
-#pragma unroll
-            for (int o = V / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const int ex = max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100) - 7;  // (rows of zeros: any will do)
-            const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float y0 = x[2 * j] * up, y1 = x[2 * j + 1] * up;
-              hi[j] = e4m3x2(y0, y1);
-              const float2 h = from_e4m3x2(hi[j]);
-              lo[j] = e4m3x2(y0 - h.x, y1 - h.y);
-            }
-            uint8_t* q = sm.q[r / kTile][0] + swizzled<D>(r % kTile, e * 8);
-            *reinterpret_cast<uint2*>(q) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-            *reinterpret_cast<uint2*>(q + kTile * D) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-            if (e == 0) sm.qscale[r] = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23) * a.scale_log2;
-          }
-        }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.q_full);
-        ++items;
-      }
-      const int pages = (walk.g.s1 - walk.g.s0) * (shared_rows(it) ? 2 : 1);
+      const int pages = (walk.g.s1 - walk.g.s0) * (shared_rows(walk.g.it) ? 2 : 1);
       constexpr int C = D / 8, R = 128 / C;  // 8 dims of a row, rows at a time
       const int r0 = c / C, e = c % C;
       // (row & 7 and the bits of the swizzle are the same for all of a thread's rows, R apart)
@@ -447,13 +443,24 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       const int units = walk.g.s1 - walk.g.s0;
       const int row = same ? r : t * kTile + r;  // of the item
       const int lim = it.limit(a, min(row, it.rows - 1)), lim_low = it.limit(a, same ? 0 : t * kTile);
-      wait(&sm.q_full, items & 1);
-      __syncwarp();
-      const float qs = sm.qscale[row];
-      if (!same) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sm.q_free);
+      const bool mine = row < it.rows;
+      const int at = it.row0 + min(row, it.rows - 1), head = it.h * a.group + at % a.group;
+      const int64_t tok = it.first + at / a.group;
+      // the row into its two terms (nobody reads what was there: this tile's scores of the last item have been seen, and with this
+      // barrier all its rows have been written out)
+      tile_sync(t);
+      if (!same || t == 0) {
+        const float e = two_terms<D>(a.q + tok * a.ts + head * a.hs, mine, sm.q[t][0], r);
+        sm.qscale[row] = e * a.scale_log2;
+        fence_proxy_async_smem();
       }
+      __syncwarp();
+      mbar_arrive_if(&sm.q_full, lane == 0);
+      if (same) {
+        wait(&sm.q_full, items & 1);
+        __syncwarp();
+      }
+      const float qs = sm.qscale[row];
       float ref = kNone, l = 0.f;
 #pragma unroll 1
       for (int u = 0; u < units; ++u, ++n) {
@@ -522,6 +529,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       __syncwarp();
       tc_fence_after();
       ++items;
+      if (same) tiles_sync();  // (`other` lies where the queries are: both tiles have all their scores)
       float down = 1.f, take = 0.f;  // what this tile's O counts, and the other's
       if (same) {
         if (t == 1) {
@@ -536,9 +544,8 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           sm.other_ref[r] = ref;
           sm.other_sum[r] = l;
           __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.other_full);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&sm.q_free);
+          mbar_arrive_if(&sm.other_full, lane == 0);
+          tiles_sync();  // (`other` has been read)
           continue;
         }
         wait(&sm.other_full, merges & 1);
@@ -550,12 +557,13 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         l = fmaf(sm.other_sum[r], take, l * down);
         ref = to;
       }
-      const bool whole = walk.g.whole();
-      const bool real = row < it.rows && ok;
+      const bool whole = walk.g.whole(), real = mine && ok;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const int at = it.row0 + min(row, it.rows - 1), head = it.h * a.group + at % a.group;
-      const int64_t tok = it.first + at / a.group;
       float* part = part_of<D>(w, walk.g.slot(), t);
+      __nv_bfloat16* out = a.out + tok * a.ots + head * a.ohs;
+      // Whole rows go through shared memory, where the tile's queries were, so that lanes next to each other write next to each
+      // other (`other` leaves no place for that).
+      uint8_t* rows = sm.q[t][0] + (warp & 3) * (32 * D * 2);
 #pragma unroll 1
       for (int i = 0; i < D; i += 32) {
         uint32_t o[32];
@@ -565,20 +573,33 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
 #pragma unroll
           for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(sm.other[i + j][r], take, __uint_as_float(o[j]) * down));
         }
-        if (real && whole) {
+        if (whole) {
 #pragma unroll
           for (int j = 0; j < 32; j += 8) {
             uint32_t y[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
               y[k] = pack_bf16(__uint_as_float(o[j + 2 * k]) * inv, __uint_as_float(o[j + 2 * k + 1]) * inv);
-            *reinterpret_cast<uint4*>(a.out + tok * a.ots + head * a.ohs + i + j) = make_uint4(y[0], y[1], y[2], y[3]);
+            const uint4 v = make_uint4(y[0], y[1], y[2], y[3]);
+            if (!same) *reinterpret_cast<uint4*>(rows + lane * (D * 2) + ((((i + j) / 8) ^ (lane & 7)) << 4)) = v;
+            else if (real) *reinterpret_cast<uint4*>(out + i + j) = v;
           }
-        }
-        if (real && !whole) {
+        } else if (real) {
 #pragma unroll
           for (int j = 0; j < 32; j += 4)
             __stcg(reinterpret_cast<uint4*>(part) + ((i + j) / 4) * kTile + r, make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+        }
+        __syncwarp();
+      }
+      if (whole && !same) {
+        constexpr int C = D / 8, R = 32 / C;  // vectors of a row, rows at a time
+        const uint32_t reals = __ballot_sync(0xffffffffu, real);
+        const int64_t from = tok * a.ots + head * a.ohs;
+#pragma unroll 4
+        for (int i = 0; i < 32; i += R) {
+          const int k = i + lane / C, v = lane % C;
+          const int64_t to = __shfl_sync(0xffffffffu, from, k);
+          if (reals >> k & 1) *reinterpret_cast<uint4*>(a.out + to + v * 8) = *reinterpret_cast<const uint4*>(rows + k * (D * 2) + ((v ^ (k & 7)) << 4));
         }
         __syncwarp();
       }
@@ -590,8 +611,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           __stcg(part + kTile * D + kTile + r, l);
         }
       }
-      __syncwarp();
-      if (same && lane == 0) mbar_arrive(&sm.q_free);
+      if (same) tiles_sync();
       if (!whole) {
         if (r == 0) sm.cut[t][n_cut & 1] = walk.g;
         ++n_cut;
@@ -617,37 +637,40 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       const int row = shared_rows(g.it) ? r : t * kTile + r;
       if (sm.last[t] && row < g.it.rows) {
         float m = kNone;
-#pragma unroll 1
+#pragma unroll 4
         for (int j = g.first_cta; j <= g.last_cta; ++j)
           m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
         const int at = g.it.row0 + row, head = g.it.h * a.group + at % a.group;
         const int64_t tok = g.it.first + at / a.group;
         float l = 0.f;
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          float4 o[D / 8];
+        for (int c = 0; c < D / 64; ++c) {  // 64 dims at a time
+          float4 o[16];
 #pragma unroll
-          for (int k = 0; k < D / 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int k = 0; k < 16; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
           l = 0.f;
 #pragma unroll 1
           for (int j = g.first_cta; j <= g.last_cta; ++j) {
             const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t);
+            float4 v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(p) + (c * 16 + k) * kTile + r);
             const float f = ex2(__ldcg(p + kTile * D + r) - m);
             l = fmaf(__ldcg(p + kTile * D + kTile + r), f, l);
 #pragma unroll
-            for (int k = 0; k < D / 8; ++k) {
-              const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + (half * (D / 8) + k) * kTile + r);
-              o[k].x = fmaf(v.x, f, o[k].x);
-              o[k].y = fmaf(v.y, f, o[k].y);
-              o[k].z = fmaf(v.z, f, o[k].z);
-              o[k].w = fmaf(v.w, f, o[k].w);
+            for (int k = 0; k < 16; ++k) {
+              o[k].x = fmaf(v[k].x, f, o[k].x);
+              o[k].y = fmaf(v[k].y, f, o[k].y);
+              o[k].z = fmaf(v[k].z, f, o[k].z);
+              o[k].w = fmaf(v[k].w, f, o[k].w);
             }
           }
           const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-          for (int k = 0; k < D / 8; ++k)
-            *reinterpret_cast<uint2*>(a.out + tok * a.ots + head * a.ohs + half * (D / 2) + k * 4) =
-                make_uint2(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv));
+          for (int k = 0; k < 16; k += 2)
+            *reinterpret_cast<uint4*>(a.out + tok * a.ots + head * a.ohs + c * 64 + k * 4) =
+                make_uint4(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv),
+                           pack_bf16(o[k + 1].x * inv, o[k + 1].y * inv), pack_bf16(o[k + 1].z * inv, o[k + 1].w * inv));
         }
         if (a.lse) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
       }
