@@ -115,65 +115,86 @@ __device__ __forceinline__ uint32_t fp16_of(uint32_t two) {
   asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\ncvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(d) : "r"(two));
   return d;
 }
-// A row of the queries as two e4m3 terms into row r of the tiles at q and behind it; returns what its values have been divided by.
+// 32 rows of the queries (row r at q_in + `from` of lane r, if it is in `there`) as two e4m3 terms into the rows from `first` on of
+// the tiles at q and behind it.  Lane r gets what its row has been divided by.  Lanes next to each other read a row together.
+// (Short code: it runs once an item, and has to come from far each time.)
 template <int D>
-__device__ __forceinline__ float two_terms(const __nv_bfloat16* from, bool there, uint8_t* q, int r) {
-  uint32_t x[D / 2];
+__device__ __forceinline__ float two_terms(const __nv_bfloat16* q_in, int64_t from, uint32_t there, uint8_t* q, int first, int lane) {
+  constexpr int C = D / 8, R = 32 / C, kAtOnce = 4;  // vectors of a row, rows at a time, loads in flight (and as many behind them)
+  const int e = lane % C, k0 = lane / C;
+  float mine = 1.f;
+  uint4 in[kAtOnce], next[kAtOnce];
+  const auto load = [&](int base) {
 #pragma unroll
-  for (int i = 0; i < D / 8; ++i) {
-    const uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(from) + i) : make_uint4(0, 0, 0, 0);
-    x[4 * i] = v.x;
-    x[4 * i + 1] = v.y;
-    x[4 * i + 2] = v.z;
-    x[4 * i + 3] = v.w;
-  }
-  uint32_t m = 0;
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int k = (base + i * R + k0) & 31;
+      const int64_t at = __shfl_sync(0xffffffffu, from, k);
+      next[i] = there >> k & 1 ? __ldg(reinterpret_cast<const uint4*>(q_in + at) + e) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  load(0);
+#pragma unroll 1
+  for (int base = 0; base < 32; base += R * kAtOnce) {
+    uint32_t top[kAtOnce];
 #pragma unroll
-  for (int i = 0; i < D / 2; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(x[i] & 0x7fff7fffu));
-  uint32_t top = max(m & 0xffffu, m >> 16);  // (as integers: NaN is above Inf)
-  if (__builtin_expect(top >= 0x7f80u, 0)) {
-    // what is not finite: NaN, which spoils the row and no other
-    top = 0;
+    for (int i = 0; i < kAtOnce; ++i) {
+      in[i] = next[i];
+      uint32_t* x = &in[i].x;
+      __nv_bfloat162 m = __float2bfloat162_rn(0.f);
 #pragma unroll
-    for (int i = 0; i < D / 2; ++i) {
-      const uint32_t lo = x[i] & 0x7fffu, hi = x[i] >> 16 & 0x7fffu;
-      top = max(top, max(lo >= 0x7f80u ? 0 : lo, hi >= 0x7f80u ? 0 : hi));
-      x[i] |= (lo >= 0x7f80u ? 0x7fffu : 0) | (hi >= 0x7f80u ? 0x7fff0000u : 0);
+      for (int j = 0; j < 4; ++j) {
+        // what is not finite: NaN, which spoils the row and no other
+        const uint32_t size = x[j] & 0x7fff7fffu;
+        const uint32_t bad = __hgeu2_mask(*reinterpret_cast<const __nv_bfloat162*>(&size), __float2bfloat162_rn(INFINITY));
+        const uint32_t good = size & ~bad;
+        x[j] |= bad & 0x7fff7fffu;
+        m = __hmax2(m, *reinterpret_cast<const __nv_bfloat162*>(&good));
+      }
+      const uint32_t two = *reinterpret_cast<uint32_t*>(&m);
+      top[i] = max(two & 0xffffu, two >> 16);
+    }
+    load(base + R * kAtOnce);
+#pragma unroll
+    for (int o = C / 2; o > 0; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const uint32_t* x = &in[i].x;
+      const int k = base + i * R + k0, ex = max(static_cast<int>(top[i] >> 7) - 127, -100) - 7;  // (rows of zeros: any will do)
+      const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // (fp16 has the 8 bits of these values, down to 2^-14, far below the last one of the second term)
+        asm("{\n"
+            ".reg .f32 a, b;\n"
+            ".reg .b32 y, z, w;\n"
+            ".reg .b16 h, l;\n"
+            "shl.b32 w, %2, 16;\n"
+            "mul.f32 a, w, %3;\n"
+            "and.b32 w, %2, 0xffff0000;\n"
+            "mul.f32 b, w, %3;\n"
+            "cvt.rn.f16x2.f32 y, b, a;\n"
+            "cvt.rn.satfinite.e4m3x2.f16x2 h, y;\n"
+            "cvt.rn.f16x2.e4m3x2 z, h;\n"
+            "sub.rn.f16x2 y, y, z;\n"
+            "cvt.rn.satfinite.e4m3x2.f16x2 l, y;\n"
+            "cvt.u32.u16 %0, h;\n"
+            "cvt.u32.u16 %1, l;\n"
+            "}\n"
+            : "=r"(hi[j]), "=r"(lo[j])
+            : "r"(x[j]), "f"(up));
+      }
+      uint8_t* at = q + swizzled<D>(first + k, e * 8);
+      *reinterpret_cast<uint2*>(at) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+      *reinterpret_cast<uint2*>(at + kTile * D) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+      // rows base + i R .. + R are in the groups of C lanes
+      const uint32_t of = __shfl_sync(0xffffffffu, 127 + ex, (lane % R) * C);
+      if (lane / R == base / R + i) mine = __uint_as_float(of << 23);
     }
   }
-  const int ex = max(static_cast<int>(top >> 7) - 127, -100) - 7;  // (rows of zeros: any will do)
-  const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-#pragma unroll
-  for (int i = 0; i < D / 8; ++i) {
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t w = x[4 * i + j];
-      // (fp16 has the 8 bits of these values, down to 2^-14, far below the last one of the second term)
-      asm("{\n"
-          ".reg .f32 a, b;\n"
-          ".reg .b32 y, z, lo32;\n"
-          ".reg .b16 h, l;\n"
-          "shl.b32 lo32, %2, 16;\n"
-          "mul.f32 a, lo32, %3;\n"
-          "and.b32 lo32, %2, 0xffff0000;\n"
-          "mul.f32 b, lo32, %3;\n"
-          "cvt.rn.f16x2.f32 y, b, a;\n"
-          "cvt.rn.satfinite.e4m3x2.f16x2 h, y;\n"
-          "cvt.rn.f16x2.e4m3x2 z, h;\n"
-          "sub.rn.f16x2 y, y, z;\n"
-          "cvt.rn.satfinite.e4m3x2.f16x2 l, y;\n"
-          "cvt.u32.u16 %0, h;\n"
-          "cvt.u32.u16 %1, l;\n"
-          "}\n"
-          : "=r"(hi[j]), "=r"(lo[j])
-          : "r"(w), "f"(up));
-    }
-    uint8_t* at = q + swizzled<D>(r, i * 8);
-    *reinterpret_cast<uint2*>(at) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-    *reinterpret_cast<uint2*>(at + kTile * D) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-  }
-  return __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+  return mine;
 }
 
 __device__ __forceinline__ void tiles_sync() { asm volatile("barrier.cta.sync 3, 256;" ::: "memory"); }
@@ -450,8 +471,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       // barrier all its rows have been written out)
       tile_sync(t);
       if (!same || t == 0) {
-        const float e = two_terms<D>(a.q + tok * a.ts + head * a.hs, mine, sm.q[t][0], r);
-        sm.qscale[row] = e * a.scale_log2;
+        sm.qscale[row] = a.scale_log2 * two_terms<D>(a.q, tok * a.ts + head * a.hs, __ballot_sync(0xffffffffu, mine), sm.q[t][0], r - lane, lane);
         fence_proxy_async_smem();
       }
       __syncwarp();
