@@ -52,7 +52,6 @@ struct ChunkSmem {
   float other_ref[kTile], other_sum[kTile];
   PageMeta meta[kMetas];
   int last[2];
-  Kv8Segment cut[2][2];                // [tile]: of the items that the run shares with others, its first and its last
   uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[kBStages], vb_empty[kBStages];
   uint64_t s_full[4], p_full[4], pv_done[4], q_full, other_full, done[2];
   uint32_t tmem;
@@ -204,6 +203,41 @@ __device__ __forceinline__ void tile_sync(int tile) { asm volatile("barrier.cta.
 template <int D>
 __device__ __forceinline__ float* part_of(const Kv8Work& w, int64_t slot, int tile) {
   return w.parts + slot * w.slot_floats + tile * (kTile * (D + 2));
+}
+
+// A row of an item that is shared by CTAs, from all their parts.
+template <int D>
+__device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w, const Kv8Segment& g, int t, int r, __nv_bfloat16* out, int64_t lse_at) {
+  float m = kNone, l = 0.f;
+  for (int j = g.first_cta; j <= g.last_cta; ++j) m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
+#pragma unroll 1
+  for (int c = 0; c < D; c += 32) {
+    float4 o[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    l = 0.f;
+#pragma unroll 1
+    for (int j = g.first_cta; j <= g.last_cta; ++j) {
+      const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t);
+      const float f = ex2(__ldcg(p + kTile * D + r) - m);
+      l = fmaf(__ldcg(p + kTile * D + kTile + r), f, l);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + (c / 4 + k) * kTile + r);
+        o[k].x = fmaf(v.x, f, o[k].x);
+        o[k].y = fmaf(v.y, f, o[k].y);
+        o[k].z = fmaf(v.z, f, o[k].z);
+        o[k].w = fmaf(v.w, f, o[k].w);
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int k = 0; k < 8; k += 2)
+      *reinterpret_cast<uint4*>(out + c + k * 4) =
+          make_uint4(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv),
+                     pack_bf16(o[k + 1].x * inv, o[k + 1].y * inv), pack_bf16(o[k + 1].z * inv, o[k + 1].w * inv));
+  }
+  if (a.lse) a.lse[lse_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 template <int D>
@@ -457,7 +491,6 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t col_o = tmem + lanes + kColO + t * 128;
     uint32_t items = 0, n = 0, kn = 0, merges = 0;  // items, units of this tile, pages before the item's first
-    int n_cut = 0;
     while (walk.next(a, w, sm.plan)) {
       const Kv8Item& it = walk.g.it;
       const bool same = shared_rows(it);
@@ -577,9 +610,43 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         l = fmaf(sm.other_sum[r], take, l * down);
         ref = to;
       }
-      const bool whole = walk.g.whole(), real = mine && ok;
+      // Is the item shared with other CTAs, then the last one of them joins the parts, in the order of the CTAs whoever that is, its
+      // own from where it is.  The others leave theirs in the workspace.
+      const Kv8Segment& g = walk.g;
+      const bool real = mine && ok;
+      const int others = g.last_cta - g.first_cta;
+      int32_t* ticket = w.tickets + 2 * g.first_cta + t;
+      bool joins = false;
+      if (others) {
+        if (r == 0) {
+          int32_t there;
+          asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(there) : "l"(ticket) : "memory");
+          if (there == others) *ticket = 0;
+          sm.last[t] = there == others;
+        }
+        tile_sync(t);
+        joins = sm.last[t];
+      }
+      const bool writes = !others || joins;  // the item's rows, else a part
+      float own = 1.f;                       // what this CTA's O counts
+      if (joins) {
+        float m = ref;
+#pragma unroll 4
+        for (int j = g.first_cta; j <= g.last_cta; ++j)
+          if (j != static_cast<int>(blockIdx.x)) m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
+        own = ex2(ref - m);
+        float sum = 0.f;
+#pragma unroll 1
+        for (int j = g.first_cta; j <= g.last_cta; ++j) {
+          const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r;
+          const bool here = j == static_cast<int>(blockIdx.x);
+          sum = fmaf(here ? l : __ldcg(p + kTile), here ? own : ex2(__ldcg(p) - m), sum);
+        }
+        l = sum;
+        ref = m;
+      }
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      float* part = part_of<D>(w, walk.g.slot(), t);
+      float* part = part_of<D>(w, g.slot(), t);
       __nv_bfloat16* out = a.out + tok * a.ots + head * a.ohs;
       // Whole rows go through shared memory, where the tile's queries were, so that lanes next to each other write next to each
       // other (`other` leaves no place for that).
@@ -593,7 +660,34 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
 #pragma unroll
           for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(sm.other[i + j][r], take, __uint_as_float(o[j]) * down));
         }
-        if (whole) {
+        if (joins) {
+          float sum[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) sum[k] = 0.f;
+#pragma unroll 1
+          for (int j = g.first_cta; j <= g.last_cta; ++j) {
+            if (j == static_cast<int>(blockIdx.x)) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) sum[k] = fmaf(__uint_as_float(o[k]), own, sum[k]);
+              continue;
+            }
+            const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t);
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(p) + (i / 4 + k) * kTile + r);
+            const float f = ex2(__ldcg(p + kTile * D + r) - ref);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              sum[4 * k] = fmaf(v[k].x, f, sum[4 * k]);
+              sum[4 * k + 1] = fmaf(v[k].y, f, sum[4 * k + 1]);
+              sum[4 * k + 2] = fmaf(v[k].z, f, sum[4 * k + 2]);
+              sum[4 * k + 3] = fmaf(v[k].w, f, sum[4 * k + 3]);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(sum[k]);
+        }
+        if (writes) {
 #pragma unroll
           for (int j = 0; j < 32; j += 8) {
             uint32_t y[4];
@@ -611,7 +705,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         }
         __syncwarp();
       }
-      if (whole && !same) {
+      if (writes && !same) {
         constexpr int C = D / 8, R = 32 / C;  // vectors of a row, rows at a time
         const uint32_t reals = __ballot_sync(0xffffffffu, real);
         const int64_t from = tok * a.ots + head * a.ohs;
@@ -624,7 +718,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         __syncwarp();
       }
       if (real) {
-        if (whole) {
+        if (writes) {
           if (a.lse) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
         } else {
           __stcg(part + kTile * D + r, ref);
@@ -632,67 +726,20 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         }
       }
       if (same) tiles_sync();
-      if (!whole) {
-        if (r == 0) sm.cut[t][n_cut & 1] = walk.g;
-        ++n_cut;
-      }
-    }
-    // ---- items that other CTAs have parts of: the last one to get here joins them
-#pragma unroll 1
-    for (int i = 0; i < n_cut; ++i) {
-      tile_sync(t);
-      const Kv8Segment& g = sm.cut[t][i];
-      if (r == 0) {
-        bool last = false;
-        if (ok) {  // (what the tile has written before the barrier goes before, what it reads behind it comes after)
-          int32_t* at = w.tickets + 2 * g.first_cta + t;
-          int32_t ticket;
-          asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(ticket) : "l"(at) : "memory");
-          last = ticket == g.last_cta - g.first_cta;
-          if (last) *at = 0;
-        }
-        sm.last[t] = last;
-      }
-      tile_sync(t);
-      const int row = shared_rows(g.it) ? r : t * kTile + r;
-      if (sm.last[t] && row < g.it.rows) {
-        float m = kNone;
-#pragma unroll 4
-        for (int j = g.first_cta; j <= g.last_cta; ++j)
-          m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
-        const int at = g.it.row0 + row, head = g.it.h * a.group + at % a.group;
-        const int64_t tok = g.it.first + at / a.group;
-        float l = 0.f;
-#pragma unroll 1
-        for (int c = 0; c < D / 64; ++c) {  // 64 dims at a time
-          float4 o[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          l = 0.f;
-#pragma unroll 1
-          for (int j = g.first_cta; j <= g.last_cta; ++j) {
-            const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t);
-            float4 v[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(p) + (c * 16 + k) * kTile + r);
-            const float f = ex2(__ldcg(p + kTile * D + r) - m);
-            l = fmaf(__ldcg(p + kTile * D + kTile + r), f, l);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-              o[k].x = fmaf(v[k].x, f, o[k].x);
-              o[k].y = fmaf(v[k].y, f, o[k].y);
-              o[k].z = fmaf(v[k].z, f, o[k].z);
-              o[k].w = fmaf(v[k].w, f, o[k].w);
-            }
+      if (!writes) {
+        tile_sync(t);
+        if (r == 0) {
+          bool last = false;
+          if (ok) {  // (what the tile has written before the barrier goes before, what it reads behind it comes after)
+            int32_t before;
+            asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(ticket) : "memory");
+            last = before == others;
+            if (last) *ticket = 0;
           }
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-          for (int k = 0; k < 16; k += 2)
-            *reinterpret_cast<uint4*>(a.out + tok * a.ots + head * a.ohs + c * 64 + k * 4) =
-                make_uint4(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv),
-                           pack_bf16(o[k + 1].x * inv, o[k + 1].y * inv), pack_bf16(o[k + 1].z * inv, o[k + 1].w * inv));
+          sm.last[t] = last;
         }
-        if (a.lse) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+        tile_sync(t);
+        if (sm.last[t] && real) join_parts<D>(a, w, g, t, r, out, tok * a.Hq + head);  // (the last of the others came meanwhile)
       }
     }
   }
