@@ -774,7 +774,7 @@ cudaError_t launch_kv8_chunk(const Kv8AttendArgs& a, Kv8Work w, int D, int ctas,
   w.step_pages = 1;
   w.half_rows = kTile;
   w.min_steps = 8;
-  w.item_steps = 4;
+  w.item_steps = 8;
   w.slot_floats = static_cast<int64_t>(kv8_chunk_slot(D));
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(ctas);

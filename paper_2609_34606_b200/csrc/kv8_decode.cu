@@ -18,8 +18,8 @@
 // scales, and one page with a large value would cost the weights of all others their low bits.)
 //
 // Warps: 0 loads pages, 1 issues the first products and 3 the second ones (one thread for both spends 1600 cycles a step on
-// looking at barriers and issuing, the loads of a step take 1400), 2 prepares the rows of Q of the next item, then one or two
-// groups of four for softmax and output.  Two groups take the steps in turn, each with sums and references of its own, which they bring
+// looking at barriers and issuing, the loads of a step take 1400), 2 prepares the rows of Q of the next item, then two
+// groups of four for softmax and output, which take the steps in turn, each with sums and references of its own, which they bring
 // together at an item's end; the group that had the item's last step writes it, while the other goes on.
 #include "kv8.cuh"
 #include "kv8_mma.cuh"
@@ -35,11 +35,11 @@ constexpr float kSlack = 1.75f; // ... and may grow to 2^8.75 < 448 before it is
 template <int D, int R>
 struct DecodeShape {
   static constexpr int N = R < 8 ? 16 : 2 * R;           // columns of the products: first terms, then second ones (16 at least)
-  static constexpr int kGroups = R <= 16 ? 2 : 1;        // (32 rows: the registers of four warps)
+  static constexpr int kGroups = 2;
   static constexpr int kThreads = 128 + 128 * kGroups;
   static constexpr int kPage = kBlock * D;               // bytes of a page tile
   static constexpr int kStage = 2 * kPage;               // of K or of V of a step
-  static constexpr int kStages = (R == 32 ? 5 : 6) * (D == 64 ? 2 : 1);
+  static constexpr int kStages = D == 64 ? 12 : 6;
   static constexpr uint32_t kS = 0;                      // TMEM columns: S of two steps, then O of their pages
   static constexpr uint32_t kO = 2 * N;
   static constexpr uint32_t kCols = 6 * N <= 128 ? 128 : 6 * N <= 256 ? 256 : 512;
@@ -52,7 +52,7 @@ struct DecodeSmem {
   uint8_t v[Sh::kStages][Sh::kStage];
   uint8_t p[2][Sh::N * 128];               // weights: [hi rows | lo rows][128 keys]
   uint8_t q[2][Sh::N * D];
-  float other[Sh::kGroups == 2 ? R * (D + 2) : 1];  // sums of the group that does not write the item: [R][D], references, sums of weights
+  float other[R * (D + 2)];  // sums of the group that does not write the item: [R][D], references, sums of weights
   float qscale[2][R];
   int limit[2][R];                         // tokens that a row sees
   PageMeta meta[Sh::kStages][2];
@@ -384,7 +384,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
   } else {
     // ---- softmax: a thread is a key of the tile, and a dim of the output.  After a wait that ran out the threads go on
     // with whatever is there, because they meet at barriers; the status word says that the result is none.
-    const int group = kGroups == 2 ? (warp - 4) / 4 : 0;
+    const int group = (warp - 4) / 4;
     const int w4 = warp & 3, key = w4 * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(w4 * 32) << 16;
     uint32_t n = 0, items = 0, merges = 0;
@@ -396,11 +396,11 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
       const uint32_t qb = items & 1;
       ++items;
       // steps n, n + 1, ... are this item's; every kGroups-th one is this group's
-      uint32_t j = n + (kGroups == 2 ? (n + group) & 1 : 0);
+      uint32_t j = n + ((n + group) & 1);
       const uint32_t end = n + steps;
       n = end;
-      const bool writes = kGroups == 1 || ((end - 1) & 1) == static_cast<uint32_t>(group);
-      const bool both = kGroups == 2 && steps > 1;
+      const bool writes = ((end - 1) & 1) == static_cast<uint32_t>(group);
+      const bool both = steps > 1;
       float ref[R], l[R], o[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
@@ -481,7 +481,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
           group_sync(group);  // (red is free again)
         }
         // (the buffer of P: what it held two steps ago has been multiplied before that could be added)
-        if (kGroups == 2 && added < j) add(added);
+        if (added < j) add(added);
         uint8_t* p = sm.p[b];
 #pragma unroll
         for (int r = 0; r < R; r += 2) {
@@ -497,7 +497,6 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         }
         fence_proxy_async_smem();
         mbar_arrive(&sm.p_full[b]);
-        if (added < j) add(added);
         vs0 = vs0_now;
         vs1 = vs1_now;
       }
@@ -638,21 +637,19 @@ cudaError_t launch_dim(const Kv8AttendArgs& a, const Kv8Work& w, int ctas, const
   return rows <= 2    ? launch_one<D, 2>(a, w, rows, ctas, tm_k, tm_v, st)
          : rows <= 4  ? launch_one<D, 4>(a, w, rows, ctas, tm_k, tm_v, st)
          : rows <= 8  ? launch_one<D, 8>(a, w, rows, ctas, tm_k, tm_v, st)
-         : rows <= 16 ? launch_one<D, 16>(a, w, rows, ctas, tm_k, tm_v, st)
-                      : launch_one<D, 32>(a, w, rows, ctas, tm_k, tm_v, st);
+                      : launch_one<D, 16>(a, w, rows, ctas, tm_k, tm_v, st);
 }
 
 }  // namespace
 
-int kv8_decode_rows(int) { return 32; }
-size_t kv8_decode_slot(int D) { return static_cast<size_t>(32) * (D + 2); }
+int kv8_decode_rows(int) { return 16; }
+size_t kv8_decode_slot(int D) { return static_cast<size_t>(16) * (D + 2); }
 
 cudaError_t kv8_decode_init(int D) {
   cudaError_t e = D == 128 ? init_one<128, 2>() : init_one<64, 2>();
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 4>() : init_one<64, 4>();
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 8>() : init_one<64, 8>();
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 16>() : init_one<64, 16>();
-  if (e == cudaSuccess) e = D == 128 ? init_one<128, 32>() : init_one<64, 32>();
   return e;
 }
 
