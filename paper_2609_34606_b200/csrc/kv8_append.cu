@@ -3,8 +3,11 @@
 // For the 64 rows of one (block, key head): x = rotated key or value, scale = 2^s with s least such that
 // max |x| <= 448 * 2^s, code = e4m3(x / scale).  Dividing by a power of two is exact, so a value is rounded once.
 //
-// It has to read 2 bytes and write 1 for every value; everything between stays on the SM.  One CTA takes a block and a
-// few heads: the sines of the block's 64 positions are worked out once, into shared memory, and serve all of them.
+// It has to read 2 bytes and write 1 for every value; everything between stays on the SM.  One CTA takes a block and a few
+// heads.  The sines of the block's 64 positions are worked out once, into shared memory, while the first head's rows are on their
+// way, and serve all heads; a head's rows are loaded while those of the head before it are turned and rounded, in registers; and
+// one barrier a head does for the maxima of keys and values, the partners of the next head's half layout, and the sums of the last
+// head's keys.  (With four barriers a head and nothing in flight across them 31 us instead of XXX for 4680 tokens, 12 heads of 128.)
 #include <cuda_fp8.h>
 
 #include "kv8.cuh"
@@ -13,7 +16,10 @@ namespace hsa {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;  // (256 with twice the rows each: twice the code, most of whose time is its way from memory in small calls)
+
+// what keys become; kHalfOdd: halves that are no whole vectors
+enum { kPlain, kInterleaved, kHalf, kHalfOdd };
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -36,31 +42,45 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t two) {
 }
 
 // What is stored of a value: NaN as 0, what passes 2^60 as 2^60.
-__device__ __forceinline__ float storable(float x, bool* bad) {
-  if (!(fabsf(x) <= kTop8)) {
-    *bad = true;
-    return x != x ? 0.f : copysignf(kTop8, x);
-  }
-  return x;
+__device__ __forceinline__ float storable(float x) { return x != x ? 0.f : fminf(fmaxf(x, -kTop8), kTop8); }
+
+__device__ __forceinline__ uint2 codes(const float (&x)[8], float inv) {
+  return make_uint2(e4m3x2(x[0] * inv, x[1] * inv) | e4m3x2(x[2] * inv, x[3] * inv) << 16,
+                    e4m3x2(x[4] * inv, x[5] * inv) | e4m3x2(x[6] * inv, x[7] * inv) << 16);
 }
+__device__ __forceinline__ void values(uint2 c, float (&x)[8]) {
+  const float2 a = from_e4m3x2(c.x & 0xffffu), b = from_e4m3x2(c.x >> 16), d = from_e4m3x2(c.y & 0xffffu), e = from_e4m3x2(c.y >> 16);
+  x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = d.x; x[5] = d.y; x[6] = e.x; x[7] = e.y;
+}
+__device__ __forceinline__ uint32_t pack(float lo, float hi) { return __float_as_uint(lo) >> 16 | (__float_as_uint(hi) & 0xffff0000u); }
 
 template <int D>
 struct AppendSmem {
-  float2 cs[kBlock][D / 2];        // cos, sin of the rows' pairs
-  uint4 raw[kBlock][D / 8];        // the keys as they came (partners of the half layout)
-  float sum[kThreads / (D / 8)][D];
-  float top[kThreads / 32];
+  float2 cs[kBlock][D / 2];               // cos, sin of the rows' pairs
+  uint4 raw[2][kBlock][D / 8];            // the keys as they came (partners of the half layout), of this head and the next
+  float sum[2][kThreads / 32][D];         // a warp's rows
+  float top[2][2][kThreads / 32];         // [head parity][keys, values]
 };
 
-// One thread: a vector of 8 dims of every (256 / (D / 8))-th row.
-template <int D>
-__global__ void __launch_bounds__(kThreads) kv8_append_kernel(const Kv8AppendArgs a) {
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void unpack(uint4 w, float (&x)[8]) {
+  x[0] = bf_lo(w.x); x[1] = bf_hi(w.x); x[2] = bf_lo(w.y); x[3] = bf_hi(w.y);
+  x[4] = bf_lo(w.z); x[5] = bf_hi(w.z); x[6] = bf_lo(w.w); x[7] = bf_hi(w.w);
+}
+
+// One thread: a vector of 8 dims of every (512 / (D / 8))-th row.
+template <int D, int MODE>
+__global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8AppendArgs a) {
   constexpr int U = D / 8;             // vectors of a row
   constexpr int R = kThreads / U;      // rows at a time
   constexpr int I = kBlock / R;        // rows of a thread
   extern __shared__ __align__(16) uint8_t smem_raw[];
   AppendSmem<D>& sm = *reinterpret_cast<AppendSmem<D>*>(smem_raw);
-  const int tid = threadIdx.x, u = tid % U, row0 = tid / U;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32, u = tid % U, row0 = tid / U;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // which block of which sequence
@@ -79,162 +99,235 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(const Kv8AppendArg
   if (t0 >= end || n == 0) return;
   const int r0 = held > t0 ? static_cast<int>(held - t0) : 0;                       // first row of this call
   const int r1 = end - t0 < kBlock ? static_cast<int>(end - t0) : kBlock;           // behind its last
-  const int page = __ldg(a.table + static_cast<int64_t>(b) * a.max_blocks + blk);
-  if (page < 0 || page >= a.max_pages) {
-    if (tid == 0) kv8_flag(a.status, kDevBounds);
-    return;
-  }
   const int64_t src0 = first + (t0 - held);  // row of the tensors at row 0 of the block (rows r0.. are there)
-  if (a.has_rope) {
+  const int h0 = blockIdx.y * a.heads, h_end = min(h0 + a.heads, a.H);
+  constexpr bool swaps = MODE == kHalf || MODE == kHalfOdd;  // partners are in other threads' vectors
+  const auto is_new = [&](int i) { return row0 + i * R >= r0 && row0 + i * R < r1; };
+  uint4 kx[I], vx[I];
+  const auto load = [&](int h) {
+    const int64_t at = src0 * a.ts + h * a.hs + u * 8;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      kx[i] = vx[i] = make_uint4(0, 0, 0, 0);
+      if (is_new(i)) {
+        kx[i] = __ldg(reinterpret_cast<const uint4*>(a.k + at + (row0 + i * R) * a.ts));
+        vx[i] = __ldg(reinterpret_cast<const uint4*>(a.v + at + (row0 + i * R) * a.ts));
+      }
+    }
+  };
+  load(h0);
+  const int page = __ldg(a.table + static_cast<int64_t>(b) * a.max_blocks + blk);
+  if constexpr (MODE != kPlain) {
     // A row's pairs side by side in threads: one position, consecutive frequencies.
     for (int i = tid; i < (r1 - r0) * a.rope.half; i += kThreads) {
       const int r = r0 + i / a.rope.half, p = i % a.rope.half;
       sm.cs[r][p] = rope_cos_sin(a.rope, p, src0 + r, static_cast<int32_t>(t0 + r));
     }
+    if constexpr (swaps) {
+#pragma unroll
+      for (int i = 0; i < I; ++i) sm.raw[0][row0 + i * R][u] = kx[i];
+    }
+    __syncthreads();
+  }
+  if (page < 0 || page >= a.max_pages) {
+    if (tid == 0) kv8_flag(a.status, kDevBounds);
+    return;
   }
   bool bad = false;
-  const int h_end = min(static_cast<int>(blockIdx.y + 1) * a.heads, a.H);
-  for (int h = blockIdx.y * a.heads; h < h_end; ++h) {
+  const bool sums = a.ksum != nullptr;
+  // the sum of the keys of the head before h, whose warps' sums a barrier has let through
+  const auto put_sum = [&](int h) {
+    if (tid < D) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < kThreads / 32; ++i) s += sm.sum[(h - h0) & 1][i][tid];
+      a.ksum[((static_cast<int64_t>(b) * a.H + h) * a.max_blocks + blk) * D + tid] = s;
+    }
+  };
+#pragma unroll 1
+  for (int h = h0; h < h_end; ++h) {
+    const int par = (h - h0) & 1;
     const int64_t ph = static_cast<int64_t>(page) * a.H + h;
-    const __nv_bfloat16* ksrc = a.k + src0 * a.ts + h * a.hs + u * 8;
-    const __nv_bfloat16* vsrc = a.v + src0 * a.ts + h * a.hs + u * 8;
-    uint4 kx[I], vx[I];
+    const float old_k = r0 > 0 ? a.k_scale[ph] : 0.f, old_v = r0 > 0 ? a.v_scale[ph] : 0.f;
+    float x[I][8];                     // keys as they are stored
+    uint4 v[I];
+    float top_k = 0.f, top_v = 0.f;
+    uint32_t most = 0;                 // of the values, as pairs of bf16
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       const int r = row0 + i * R;
-      kx[i] = vx[i] = make_uint4(0, 0, 0, 0);
-      if (r >= r0 && r < r1) {
-        kx[i] = __ldg(reinterpret_cast<const uint4*>(ksrc + r * a.ts));
-        vx[i] = __ldg(reinterpret_cast<const uint4*>(vsrc + r * a.ts));
-      }
-    }
-    if (a.has_rope && !a.rope.interleaved) {
+      unpack(kx[i], x[i]);
+      v[i] = vx[i];
+      if (MODE != kPlain && is_new(i)) {
+        if constexpr (MODE == kInterleaved) {
 #pragma unroll
-      for (int i = 0; i < I; ++i) sm.raw[row0 + i * R][u] = kx[i];
-    }
-    __syncthreads();  // (sines and raw keys are there)
-#pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
-      const bool is_k = which == 0;
-      float x[I][8];
-      float top = 0.f;
+          for (int j = 0; j < 4; ++j)
+            if (u * 4 + j < a.rope.half) {
+              const float2 cs = sm.cs[r][u * 4 + j];
+              const float va = x[i][2 * j], vb = x[i][2 * j + 1];
+              x[i][2 * j] = fmaf(va, cs.x, -(vb * cs.y));
+              x[i][2 * j + 1] = fmaf(vb, cs.x, va * cs.y);
+            }
+        } else if constexpr (MODE == kHalf) {
+          const int hv = a.rope.half / 8;
+          if (u < 2 * hv) {
+            float y[8];
+            unpack(sm.raw[par][r][u < hv ? u + hv : u - hv], y);
+            const float2* cs = &sm.cs[r][(u < hv ? u : u - hv) * 8];
+            const float sign = u < hv ? -1.f : 1.f;
 #pragma unroll
-      for (int i = 0; i < I; ++i) {
-        const int r = row0 + i * R;
-        const uint4 w = is_k ? kx[i] : vx[i];
-        x[i][0] = bf_lo(w.x); x[i][1] = bf_hi(w.x); x[i][2] = bf_lo(w.y); x[i][3] = bf_hi(w.y);
-        x[i][4] = bf_lo(w.z); x[i][5] = bf_hi(w.z); x[i][6] = bf_lo(w.w); x[i][7] = bf_hi(w.w);
-        if (is_k && a.has_rope && r >= r0 && r < r1) {
-          if (a.rope.interleaved) {
+            for (int j = 0; j < 8; ++j) x[i][j] = fmaf(x[i][j], cs[j].x, sign * (y[j] * cs[j].y));
+          }
+        } else {
+          const __nv_bfloat16* raw = reinterpret_cast<const __nv_bfloat16*>(&sm.raw[par][r][0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (u * 4 + j < a.rope.half) {
-                const float2 cs = sm.cs[r][u * 4 + j];
-                const float va = x[i][2 * j], vb = x[i][2 * j + 1];
-                x[i][2 * j] = fmaf(va, cs.x, -(vb * cs.y));
-                x[i][2 * j + 1] = fmaf(vb, cs.x, va * cs.y);
-              }
-          } else {
-            const __nv_bfloat16* raw = reinterpret_cast<const __nv_bfloat16*>(&sm.raw[r][0]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const int dim = u * 8 + j;
-              if (dim < a.rope.half) {
-                const float2 cs = sm.cs[r][dim];
-                x[i][j] = fmaf(x[i][j], cs.x, -(__bfloat162float(raw[dim + a.rope.half]) * cs.y));
-              } else if (dim < 2 * a.rope.half) {
-                const float2 cs = sm.cs[r][dim - a.rope.half];
-                x[i][j] = fmaf(x[i][j], cs.x, __bfloat162float(raw[dim - a.rope.half]) * cs.y);
-              }
+          for (int j = 0; j < 8; ++j) {
+            const int dim = u * 8 + j;
+            if (dim < 2 * a.rope.half) {
+              const bool first = dim < a.rope.half;
+              const float2 cs = sm.cs[r][first ? dim : dim - a.rope.half];
+              const float y = __bfloat162float(raw[first ? dim + a.rope.half : dim - a.rope.half]);
+              x[i][j] = fmaf(x[i][j], cs.x, (first ? -1.f : 1.f) * (y * cs.y));
             }
           }
         }
+      }
+      // (maxima that keep NaN)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top_k) : "f"(fabsf(x[i][j])));
+      const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(most) : "r"(w[j] & 0x7fff7fffu));
+    }
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(top_v) : "f"(bf_lo(most)), "f"(bf_hi(most)));
+    if (h + 1 < h_end) {
+      load(h + 1);
+      if constexpr (swaps) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) sm.raw[par ^ 1][row0 + i * R][u] = kx[i];
+      }
+    }
+    const auto meet = [&]() {  // the maxima of the CTA
+      top_k = warp_max(top_k);
+      top_v = warp_max(top_v);
+      if (lane == 0) {
+        sm.top[par][0][warp] = top_k;
+        sm.top[par][1][warp] = top_v;
+      }
+      __syncthreads();  // (also: everybody has read the old scales, and the last head's sums are there)
+      top_k = warp_max(sm.top[par][0][lane % (kThreads / 32)]);
+      top_v = warp_max(sm.top[par][1][lane % (kThreads / 32)]);
+    };
+    meet();
+    if (__builtin_expect(!(top_k <= kTop8) || !(top_v <= kTop8), 0)) {
+      // something that cannot be stored as it is
+      __syncthreads();  // (the maxima have been read)
+      top_k = top_v = 0.f;
+      bad = true;
+#pragma unroll
+      for (int i = 0; i < I; ++i) {
+        float y[8];
+        unpack(v[i], y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          x[i][j] = storable(x[i][j], &bad);
-          top = fmaxf(top, fabsf(x[i][j]));
+          x[i][j] = storable(x[i][j]);
+          y[j] = storable(y[j]);
+          top_k = fmaxf(top_k, fabsf(x[i][j]));
+          top_v = fmaxf(top_v, fabsf(y[j]));
+        }
+        v[i] = make_uint4(pack(y[0], y[1]), pack(y[2], y[3]), pack(y[4], y[5]), pack(y[6], y[7]));  // (exact)
+      }
+      meet();
+    }
+    if (sums && h > h0) put_sum(h - 1);
+    const float scale_k = fmaxf(pow2(scale_exponent(top_k)), old_k), scale_v = fmaxf(pow2(scale_exponent(top_v)), old_v);
+    const float inv_k = 1.f / scale_k, inv_v = 1.f / scale_v;
+    if (tid == 0) {
+      a.k_scale[ph] = scale_k;
+      a.v_scale[ph] = scale_v;
+    }
+    const int64_t to = ph * (kBlock * D) + u * 8;
+    float sum[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+      if (!is_new(i) && r0 > 0) continue;  // (rows behind the last one of a block that begins here: zeros)
+      const int64_t at = to + (row0 + i * R) * D;
+      float y[8];
+      unpack(v[i], y);
+      *reinterpret_cast<uint2*>(a.k_pool + at) = codes(x[i], inv_k);
+      *reinterpret_cast<uint2*>(a.v_pool + at) = codes(y, inv_v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += x[i][j];
+    }
+    if (r0 > 0 && (scale_k > old_k || scale_v > old_v || sums)) {
+      // rows of earlier calls, and those behind the last: their codes follow a scale that has grown
+#pragma unroll 1
+      for (int job = 0; job < 2 * I; ++job) {
+        const bool is_k = job < I;
+        const int r = row0 + (is_k ? job : job - I) * R;
+        const float old_scale = is_k ? old_k : old_v, scale = is_k ? scale_k : scale_v;
+        const bool summed = is_k && sums && r < r0;
+        if ((r >= r0 && r < r1) || !(scale > old_scale || summed)) continue;
+        const float shrink = old_scale * (is_k ? inv_k : inv_v);
+        uint2* at = reinterpret_cast<uint2*>((is_k ? a.k_pool : a.v_pool) + to + r * D);
+        const uint2 c = *at;
+        float y[8];
+        values(c, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] *= shrink;
+        const uint2 now = codes(y, 1.f);
+        if (scale > old_scale) *at = now;
+        if (summed) {
+          values(now, y);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[j] = fmaf(y[j], scale, sum[j]);
         }
       }
+    }
+    if (sums) {
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if ((tid & 31) == 0) sm.top[tid / 32] = top;
-      uint8_t* codes = (is_k ? a.k_pool : a.v_pool) + ph * (kBlock * D) + u * 8;
-      float* scale_at = (is_k ? a.k_scale : a.v_scale) + ph;
-      const float old_scale = r0 > 0 ? *scale_at : 0.f;
-      __syncthreads();  // (also: everybody has read the old scale)
+      for (int j = 0; j < 8; ++j) {
 #pragma unroll
-      for (int i = 0; i < kThreads / 32; ++i) top = fmaxf(top, sm.top[i]);
-      const float scale = fmaxf(pow2(scale_exponent(top)), old_scale), inv = 1.f / scale;
-      if (tid == 0) *scale_at = scale;
-      const bool grown = r0 > 0 && scale > old_scale;
-      const float shrink = r0 > 0 ? old_scale * inv : 0.f;
-      const bool sums = is_k && a.ksum != nullptr;
-      float sum[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-#pragma unroll
-      for (int i = 0; i < I; ++i) {
-        const int r = row0 + i * R;
-        uint2* at = reinterpret_cast<uint2*>(codes + r * D);
-        if ((r >= r0 && r < r1) || r0 == 0) {
-          uint2 c;
-          c.x = e4m3x2(x[i][0] * inv, x[i][1] * inv) | e4m3x2(x[i][2] * inv, x[i][3] * inv) << 16;
-          c.y = e4m3x2(x[i][4] * inv, x[i][5] * inv) | e4m3x2(x[i][6] * inv, x[i][7] * inv) << 16;
-          *at = c;
-          if (sums)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += x[i][j];
-        } else if (grown || (sums && r < r0)) {
-          // rows of earlier calls: their codes follow a grown scale
-          const uint2 c = *at;
-          const uint32_t w[2] = {c.x, c.y};
-          uint32_t y[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float2 lo = from_e4m3x2(w[j] & 0xffffu), hi = from_e4m3x2(w[j] >> 16);
-            y[j] = e4m3x2(lo.x * shrink, lo.y * shrink) | e4m3x2(hi.x * shrink, hi.y * shrink) << 16;
-            if (sums && r < r0) {
-              const float2 l2 = from_e4m3x2(y[j] & 0xffffu), h2 = from_e4m3x2(y[j] >> 16);
-              sum[4 * j] = fmaf(l2.x, scale, sum[4 * j]);
-              sum[4 * j + 1] = fmaf(l2.y, scale, sum[4 * j + 1]);
-              sum[4 * j + 2] = fmaf(h2.x, scale, sum[4 * j + 2]);
-              sum[4 * j + 3] = fmaf(h2.y, scale, sum[4 * j + 3]);
-            }
-          }
-          if (grown) *at = make_uint2(y[0], y[1]);
-        }
+        for (int o = U; o < 32; o <<= 1) sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], o);
+        if (lane < U) sm.sum[par][warp][u * 8 + j] = sum[j];
       }
-      if (sums) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sm.sum[row0][u * 8 + j] = sum[j];
-        __syncthreads();
-        if (tid < D) {
-          float s = 0.f;
-#pragma unroll
-          for (int i = 0; i < R; ++i) s += sm.sum[i][tid];
-          a.ksum[((static_cast<int64_t>(b) * a.H + h) * a.max_blocks + blk) * D + tid] = s;
-        }
-      }
-      __syncthreads();  // (sm.top, sm.sum and, behind the keys, sm.raw are free again)
     }
   }
-  if (bad) kv8_flag(a.status, kDevNonfinite);
+  if (sums) {
+    __syncthreads();
+    put_sum(h_end - 1);
+  }
+  if (bad && tid == 0) kv8_flag(a.status, kDevNonfinite);
 }
 
 }  // namespace
 
+namespace {
+
+using AppendKernel = void (*)(Kv8AppendArgs);
+template <int D>
+constexpr AppendKernel kKernels[4] = {kv8_append_kernel<D, kPlain>, kv8_append_kernel<D, kInterleaved>, kv8_append_kernel<D, kHalf>,
+                                      kv8_append_kernel<D, kHalfOdd>};
+
+}  // namespace
+
 cudaError_t kv8_append_init(int D) {
-  return D == 128 ? cudaFuncSetAttribute(kv8_append_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(AppendSmem<128>))
-                  : cudaFuncSetAttribute(kv8_append_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(AppendSmem<64>));
+  cudaError_t e = cudaSuccess;
+  for (int mode = 0; mode < 4 && e == cudaSuccess; ++mode)
+    e = cudaFuncSetAttribute(D == 128 ? kKernels<128>[mode] : kKernels<64>[mode], cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(D == 128 ? sizeof(AppendSmem<128>) : sizeof(AppendSmem<64>)));
+  return e;
 }
 
 cudaError_t launch_kv8_append(const Kv8AppendArgs& args, int D, int nsm, cudaStream_t st) {
   Kv8AppendArgs a = args;
   a.blocks_per_seq = (a.rows.max_rows + 2 * kBlock - 2) / kBlock;
   const int64_t blocks = static_cast<int64_t>(a.rows.batch) * a.blocks_per_seq;
-  // heads of a CTA: enough to share the sines, while three CTAs to an SM are left
-  int64_t heads = a.has_rope ? blocks * a.H / (3 * static_cast<int64_t>(nsm)) : 1;
-  a.heads = static_cast<int>(heads < 1 ? 1 : heads > 4 ? 4 : heads);
+  // Heads of a CTA: as many as leave two CTAs to an SM, at most 16: with positions they share the sines, and all share a CTA's start.
+  const int64_t heads = blocks * a.H / (2 * static_cast<int64_t>(nsm));
+  a.heads = static_cast<int>(heads < 1 ? 1 : heads > 16 ? 16 : heads);
   if (a.heads > a.H) a.heads = a.H;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(blocks), (a.H + a.heads - 1) / a.heads);
@@ -246,7 +339,8 @@ cudaError_t launch_kv8_append(const Kv8AppendArgs& args, int D, int nsm, cudaStr
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, D == 128 ? kv8_append_kernel<128> : kv8_append_kernel<64>, a);
+  const int mode = !a.has_rope ? kPlain : a.rope.interleaved ? kInterleaved : a.rope.half % 8 ? kHalfOdd : kHalf;
+  return cudaLaunchKernelEx(&cfg, D == 128 ? kKernels<128>[mode] : kKernels<64>[mode], a);
 }
 
 }  // namespace hsa
