@@ -7,7 +7,7 @@
 // heads.  The sines of the block's 64 positions are worked out once, into shared memory, while the first head's rows are on their
 // way, and serve all heads; a head's rows are loaded while those of the head before it are turned and rounded, in registers; and
 // one barrier a head does for the maxima of keys and values, the partners of the next head's half layout, and the sums of the last
-// head's keys.  (With four barriers a head and nothing in flight across them 31 us instead of XXX for 4680 tokens, 12 heads of 128.)
+// head's keys.  (With four barriers a head and nothing in flight across them 31 us instead of 18 for 4680 tokens, 12 heads of 128.)
 #include <cuda_fp8.h>
 
 #include "kv8.cuh"
@@ -16,7 +16,10 @@ namespace hsa {
 
 namespace {
 
-constexpr int kThreads = 512;  // (256 with twice the rows each: twice the code, most of whose time is its way from memory in small calls)
+// 512 for heads of 128, 256 for 64: two rows to a thread.  (More rows to a thread make more code, whose way from memory is most of
+// a small call's time; with one row to a thread too little is in flight.)
+template <int D>
+constexpr int kThreads = 4 * D;
 
 // what keys become; kHalfOdd: halves that are no whole vectors
 enum { kPlain, kInterleaved, kHalf, kHalfOdd };
@@ -33,6 +36,8 @@ __device__ __forceinline__ int scale_exponent(float top) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
 
+__device__ __forceinline__ float inverse(float scale) { return __uint_as_float((254u << 23) - __float_as_uint(scale)); }  // of a power of two
+
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   return __nv_cvt_float2_to_fp8x2(make_float2(lo, hi), __NV_SATFINITE, __NV_E4M3);
 }
@@ -44,9 +49,36 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t two) {
 // What is stored of a value: NaN as 0, what passes 2^60 as 2^60.
 __device__ __forceinline__ float storable(float x) { return x != x ? 0.f : fminf(fmaxf(x, -kTop8), kTop8); }
 
+// Where a pair's cosine and sine stand in its row.  Lanes next to each other, which have vectors next to each other, read 16 bytes
+// next to each other: the half layout has four cosines of a vector, then the same four of the next, and the sines behind; the
+// interleaved one two cosines and sines.  (A vector's in a row: four lanes of eight meet in a bank.)
+template <int D, int MODE>
+__device__ __forceinline__ int cos_at(int pair) {
+  if (MODE == kHalf) return pair % 8 / 4 * (D / 4) + pair / 8 * 4 + pair % 4;
+  if (MODE == kInterleaved) return pair % 4 / 2 * D / 2 + pair / 4 * 4 + pair % 2 * 2;
+  return 2 * pair;
+}
+template <int D, int MODE>
+__device__ __forceinline__ int sin_at(int pair) { return cos_at<D, MODE>(pair) + (MODE == kHalf ? D / 2 : 1); }
+
+// two fp32 at a time
+__device__ __forceinline__ void mul2(float& a, float& b, float c, float d) {
+  asm("{\n.reg .b64 x, y;\nmov.b64 x, {%0, %1};\nmov.b64 y, {%2, %3};\nmul.rn.f32x2 x, x, y;\nmov.b64 {%0, %1}, x;\n}\n" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
+__device__ __forceinline__ void fma2(float& a, float& b, float c, float d, float e, float f) {
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%0, %1};\nmov.b64 y, {%2, %3};\nmov.b64 z, {%4, %5};\nfma.rn.f32x2 x, x, y, z;\nmov.b64 {%0, %1}, x;\n}\n"
+      : "+f"(a), "+f"(b)
+      : "f"(c), "f"(d), "f"(e), "f"(f));
+}
 __device__ __forceinline__ uint2 codes(const float (&x)[8], float inv) {
-  return make_uint2(e4m3x2(x[0] * inv, x[1] * inv) | e4m3x2(x[2] * inv, x[3] * inv) << 16,
-                    e4m3x2(x[4] * inv, x[5] * inv) | e4m3x2(x[6] * inv, x[7] * inv) << 16);
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    y[j] = x[j];
+    y[j + 1] = x[j + 1];
+    mul2(y[j], y[j + 1], inv, inv);
+  }
+  return make_uint2(e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16, e4m3x2(y[4], y[5]) | e4m3x2(y[6], y[7]) << 16);
 }
 __device__ __forceinline__ void values(uint2 c, float (&x)[8]) {
   const float2 a = from_e4m3x2(c.x & 0xffffu), b = from_e4m3x2(c.x >> 16), d = from_e4m3x2(c.y & 0xffffu), e = from_e4m3x2(c.y >> 16);
@@ -56,10 +88,10 @@ __device__ __forceinline__ uint32_t pack(float lo, float hi) { return __float_as
 
 template <int D>
 struct AppendSmem {
-  float2 cs[kBlock][D / 2];               // cos, sin of the rows' pairs
+  float cs[kBlock][D];                    // cos, sin of the rows' pairs
   uint4 raw[2][kBlock][D / 8];            // the keys as they came (partners of the half layout), of this head and the next
-  float sum[2][kThreads / 32][D];         // a warp's rows
-  float top[2][2][kThreads / 32];         // [head parity][keys, values]
+  float sum[2][kThreads<D> / 32][D];         // a warp's rows
+  float top[2][2][kThreads<D> / 32];         // [head parity][keys, values]
 };
 
 __device__ __forceinline__ float warp_max(float x) {
@@ -72,11 +104,11 @@ __device__ __forceinline__ void unpack(uint4 w, float (&x)[8]) {
   x[4] = bf_lo(w.z); x[5] = bf_hi(w.z); x[6] = bf_lo(w.w); x[7] = bf_hi(w.w);
 }
 
-// One thread: a vector of 8 dims of every (512 / (D / 8))-th row.
+// One thread: a vector of 8 dims of every 32nd row.
 template <int D, int MODE>
-__global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8AppendArgs a) {
+__global__ void __launch_bounds__(kThreads<D>, D == 128 ? 2 : 4) kv8_append_kernel(const Kv8AppendArgs a) {
   constexpr int U = D / 8;             // vectors of a row
-  constexpr int R = kThreads / U;      // rows at a time
+  constexpr int R = kThreads<D> / U;      // rows at a time
   constexpr int I = kBlock / R;        // rows of a thread
   extern __shared__ __align__(16) uint8_t smem_raw[];
   AppendSmem<D>& sm = *reinterpret_cast<AppendSmem<D>*>(smem_raw);
@@ -119,9 +151,11 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
   const int page = __ldg(a.table + static_cast<int64_t>(b) * a.max_blocks + blk);
   if constexpr (MODE != kPlain) {
     // A row's pairs side by side in threads: one position, consecutive frequencies.
-    for (int i = tid; i < (r1 - r0) * a.rope.half; i += kThreads) {
+    for (int i = tid; i < (r1 - r0) * a.rope.half; i += kThreads<D>) {
       const int r = r0 + i / a.rope.half, p = i % a.rope.half;
-      sm.cs[r][p] = rope_cos_sin(a.rope, p, src0 + r, static_cast<int32_t>(t0 + r));
+      const float2 cs = rope_cos_sin(a.rope, p, src0 + r, static_cast<int32_t>(t0 + r));
+      sm.cs[r][cos_at<D, MODE>(p)] = cs.x;
+      sm.cs[r][sin_at<D, MODE>(p)] = cs.y;
     }
     if constexpr (swaps) {
 #pragma unroll
@@ -140,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
     if (tid < D) {
       float s = 0.f;
 #pragma unroll
-      for (int i = 0; i < kThreads / 32; ++i) s += sm.sum[(h - h0) & 1][i][tid];
+      for (int i = 0; i < kThreads<D> / 32; ++i) s += sm.sum[(h - h0) & 1][i][tid];
       a.ksum[((static_cast<int64_t>(b) * a.H + h) * a.max_blocks + blk) * D + tid] = s;
     }
   };
@@ -163,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             if (u * 4 + j < a.rope.half) {
-              const float2 cs = sm.cs[r][u * 4 + j];
+              const float2 cs = *reinterpret_cast<const float2*>(&sm.cs[r][cos_at<D, MODE>(u * 4 + j)]);
               const float va = x[i][2 * j], vb = x[i][2 * j + 1];
               x[i][2 * j] = fmaf(va, cs.x, -(vb * cs.y));
               x[i][2 * j + 1] = fmaf(vb, cs.x, va * cs.y);
@@ -173,10 +207,19 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
           if (u < 2 * hv) {
             float y[8];
             unpack(sm.raw[par][r][u < hv ? u + hv : u - hv], y);
-            const float2* cs = &sm.cs[r][(u < hv ? u : u - hv) * 8];
             const float sign = u < hv ? -1.f : 1.f;
+            const int w = (u < hv ? u : u - hv) * 8;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[i][j] = fmaf(x[i][j], cs[j].x, sign * (y[j] * cs[j].y));
+            for (int j = 0; j < 8; j += 4) {
+              const float4 c = *reinterpret_cast<const float4*>(&sm.cs[r][cos_at<D, MODE>(w + j)]);
+              const float4 d = *reinterpret_cast<const float4*>(&sm.cs[r][sin_at<D, MODE>(w + j)]);
+              mul2(y[j], y[j + 1], sign, sign);
+              mul2(y[j + 2], y[j + 3], sign, sign);
+              mul2(y[j], y[j + 1], d.x, d.y);
+              mul2(y[j + 2], y[j + 3], d.z, d.w);
+              fma2(x[i][j], x[i][j + 1], c.x, c.y, y[j], y[j + 1]);
+              fma2(x[i][j + 2], x[i][j + 3], c.z, c.w, y[j + 2], y[j + 3]);
+            }
           }
         } else {
           const __nv_bfloat16* raw = reinterpret_cast<const __nv_bfloat16*>(&sm.raw[par][r][0]);
@@ -185,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
             const int dim = u * 8 + j;
             if (dim < 2 * a.rope.half) {
               const bool first = dim < a.rope.half;
-              const float2 cs = sm.cs[r][first ? dim : dim - a.rope.half];
+              const float2 cs = *reinterpret_cast<const float2*>(&sm.cs[r][cos_at<D, MODE>(first ? dim : dim - a.rope.half)]);
               const float y = __bfloat162float(raw[first ? dim + a.rope.half : dim - a.rope.half]);
               x[i][j] = fmaf(x[i][j], cs.x, (first ? -1.f : 1.f) * (y * cs.y));
             }
@@ -194,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
       }
       // (maxima that keep NaN)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) asm("max.NaN.f32 %0, %0, %1;" : "+f"(top_k) : "f"(fabsf(x[i][j])));
+      for (int j = 0; j < 8; j += 2) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top_k) : "f"(x[i][j]), "f"(x[i][j + 1]));
       const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(most) : "r"(w[j] & 0x7fff7fffu));
@@ -215,8 +258,8 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
         sm.top[par][1][warp] = top_v;
       }
       __syncthreads();  // (also: everybody has read the old scales, and the last head's sums are there)
-      top_k = warp_max(sm.top[par][0][lane % (kThreads / 32)]);
-      top_v = warp_max(sm.top[par][1][lane % (kThreads / 32)]);
+      top_k = warp_max(sm.top[par][0][lane % (kThreads<D> / 32)]);
+      top_v = warp_max(sm.top[par][1][lane % (kThreads<D> / 32)]);
     };
     meet();
     if (__builtin_expect(!(top_k <= kTop8) || !(top_v <= kTop8), 0)) {
@@ -241,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 2) kv8_append_kernel(const Kv8Append
     }
     if (sums && h > h0) put_sum(h - 1);
     const float scale_k = fmaxf(pow2(scale_exponent(top_k)), old_k), scale_v = fmaxf(pow2(scale_exponent(top_v)), old_v);
-    const float inv_k = 1.f / scale_k, inv_v = 1.f / scale_v;
+    const float inv_k = inverse(scale_k), inv_v = inverse(scale_v);
     if (tid == 0) {
       a.k_scale[ph] = scale_k;
       a.v_scale[ph] = scale_v;
@@ -331,7 +374,7 @@ cudaError_t launch_kv8_append(const Kv8AppendArgs& args, int D, int nsm, cudaStr
   if (a.heads > a.H) a.heads = a.H;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(blocks), (a.H + a.heads - 1) / a.heads);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(D == 128 ? kThreads<128> : kThreads<64>);
   cfg.dynamicSmemBytes = D == 128 ? sizeof(AppendSmem<128>) : sizeof(AppendSmem<64>);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
