@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "rope.cuh"
@@ -13,6 +14,8 @@
 namespace hsa {
 
 namespace {
+
+constexpr int kRows = 4;  // heads in flight
 
 template <typename T>
 struct Vec {
@@ -26,13 +29,29 @@ __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__half* p, float x) { *p = __float2half_rn(x); }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
+// n / d for n < 2^31 as a product: with 2^(s - 1) < d <= 2^s and m = floor(2^(31 + s) / d) + 1, n m / 2^(31 + s) is above n / d by
+// at most n / 2^(31 + s) < 1 / d, and m is below 2^32.
+struct Divide {
+  uint32_t m;
+  int s;
+  int d;
+  __device__ __forceinline__ uint32_t operator()(uint32_t n) const { return static_cast<uint32_t>(static_cast<uint64_t>(n) * m >> s); }
+};
+Divide divide_by(int d) {
+  int s = 0;
+  while ((1ll << s) < d) ++s;
+  return Divide{static_cast<uint32_t>((1ull << (31 + s)) / d + 1), 31 + s, d};
+}
+
 struct RopeArgs {
   const void* x;
   void* out;
   int64_t ts, hs, ots, ohs;
   int H, D, heads_per_thread, head_groups;
-  int64_t threads;  // tokens * head_groups * units
+  uint32_t threads;   // of a slab of tokens: tokens * head_groups * units
+  int64_t tokens, slab;
   int units;
+  Divide by_units, by_groups;
   RopeDev rope;
 };
 
@@ -41,17 +60,16 @@ struct RopeArgs {
 //         behind those are vectors that pass through.
 // MODE 2, other halves: a unit is one pair, or one value that passes through.
 template <typename T, int MODE>
-__global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 4 : 3) rope_kernel(const RopeArgs a) {
   constexpr int N = Vec<T>::N;
-  constexpr int kRows = 4;  // heads in flight
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int64_t idx = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const uint32_t idx = blockIdx.x * 256 + threadIdx.x;
   if (idx >= a.threads) return;
-  const int u = static_cast<int>(idx % a.units);
-  const int64_t rest = idx / a.units;
-  const int hg = static_cast<int>(rest % a.head_groups);
-  const int64_t t = rest / a.head_groups;
+  const uint32_t rest = a.by_units(idx), in_slab = a.by_groups(rest);
+  const int u = static_cast<int>(idx - rest * a.units), hg = static_cast<int>(rest - in_slab * a.head_groups);
+  const int64_t t = blockIdx.y * a.slab + in_slab;
+  if (t >= a.tokens) return;
   const int h0 = hg * a.heads_per_thread, h1 = h0 + a.heads_per_thread < a.H ? h0 + a.heads_per_thread : a.H;
   const T* x = static_cast<const T*>(a.x) + t * a.ts;
   T* out = static_cast<T*>(a.out) + t * a.ots;
@@ -60,22 +78,43 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
     const bool turn = u < r.half;
     const int d0 = turn ? u : u + r.half;
     const float2 cs = turn ? rope_cos_sin(r, u, t, static_cast<int32_t>(t)) : make_float2(1.f, 0.f);
-    for (int h = h0; h < h1; ++h) {
-      const T* p = x + h * a.hs + d0;
-      T* o = out + h * a.ohs + d0;
-      if (turn) {
-        const float va = to_f(p[0]), vb = to_f(p[r.half]);
-        put(o, fmaf(va, cs.x, -(vb * cs.y)));
-        put(o + r.half, fmaf(vb, cs.x, va * cs.y));
-      } else {
-        o[0] = p[0];
-      }
+    for (int h = h0; h < h1; h += kRows) {
+      T va[kRows], vb[kRows];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (h + i < h1) {
+          const T* p = x + (h + i) * a.hs + d0;
+          va[i] = p[0];
+          if (turn) vb[i] = p[r.half];
+        }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (h + i < h1) {
+          T* o = out + (h + i) * a.ohs + d0;
+          if (turn) {
+            const float v0 = to_f(va[i]), v1 = to_f(vb[i]);
+            put(&va[i], fmaf(v0, cs.x, -(v1 * cs.y)));
+            put(o + r.half, fmaf(v1, cs.x, v0 * cs.y));
+          }
+          o[0] = va[i];
+        }
     }
     return;
   } else {
     constexpr int P = MODE == 0 ? N / 2 : N;  // pairs of a unit
     const bool turn = MODE == 0 || u * N < r.half;
     const int d0 = turn ? u * N : u * N + r.half;
+    uint4 va[kRows], vb[kRows];
+    const auto load = [&](int h) {
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (h + i < h1) {
+          const T* p = x + (h + i) * a.hs + d0;
+          va[i] = *reinterpret_cast<const uint4*>(p);
+          if (MODE == 1 && turn) vb[i] = *reinterpret_cast<const uint4*>(p + r.half);
+        }
+    };
+    load(h0);  // (on their way while the sines are worked out)
     float2 cs[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -84,14 +123,7 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
       if (pair < r.half) cs[i] = rope_cos_sin(r, pair, t, static_cast<int32_t>(t));
     }
     for (int h = h0; h < h1; h += kRows) {
-      uint4 va[kRows], vb[kRows];
-#pragma unroll
-      for (int i = 0; i < kRows; ++i)
-        if (h + i < h1) {
-          const T* p = x + (h + i) * a.hs + d0;
-          va[i] = *reinterpret_cast<const uint4*>(p);
-          if (MODE == 1 && turn) vb[i] = *reinterpret_cast<const uint4*>(p + r.half);
-        }
+      if (h > h0) load(h);
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
         if (h + i < h1) {
@@ -123,15 +155,24 @@ cudaError_t launch_rope(RopeArgs a, int64_t tokens, int nsm, cudaStream_t st) {
   const int rest = a.D - 2 * a.rope.half;
   const int mode = a.rope.interleaved ? 0 : a.rope.half % N == 0 ? 1 : 2;
   a.units = mode == 0 ? a.D / N : mode == 1 ? (a.rope.half + rest) / N : a.rope.half + rest;
-  // As many heads to a thread as leave 1024 threads to an SM, at most 16: the sines are shared by them.
+  // As many heads to a thread as leave 1024 threads to an SM, at most 4, whose loads are in flight at once: the sines are shared
+  // by them.  (At most 16: 20,011 tokens, 12 heads of 128 in bf16 32 us, for want of threads.)
   int64_t per = tokens * a.H * a.units / (static_cast<int64_t>(nsm) * 1024);
-  a.heads_per_thread = static_cast<int>(per < 1 ? 1 : per > 16 ? 16 : per);
+  a.heads_per_thread = static_cast<int>(per < 1 ? 1 : per > kRows ? kRows : per);
   if (a.heads_per_thread > a.H) a.heads_per_thread = a.H;
   a.head_groups = (a.H + a.heads_per_thread - 1) / a.heads_per_thread;
   a.heads_per_thread = (a.H + a.head_groups - 1) / a.head_groups;  // even shares
-  a.threads = tokens * a.head_groups * a.units;
+  // threads are counted in 31 bits: more tokens than that go into slabs
+  const int64_t per_token = static_cast<int64_t>(a.head_groups) * a.units;
+  a.tokens = tokens;
+  a.slab = std::min(tokens, static_cast<int64_t>((1ll << 31) - 256) / per_token);
+  a.threads = static_cast<uint32_t>(a.slab * per_token);
+  a.by_units = divide_by(a.units);
+  a.by_groups = divide_by(a.head_groups);
+  const int64_t slabs = (tokens + a.slab - 1) / a.slab;
+  if (slabs > 65535) return cudaErrorInvalidValue;  // (more than any memory holds)
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>((a.threads + 255) / 256));
+  cfg.gridDim = dim3((a.threads + 255) / 256, static_cast<unsigned>(slabs));
   cfg.blockDim = dim3(256);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
