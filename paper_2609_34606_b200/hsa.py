@@ -190,15 +190,16 @@ def _stream() -> int:
 
 def _on_current(t: torch.Tensor, name: str) -> None:
     """The calls enqueue on the current stream of the current device: refuses a tensor of another one."""
-    if t.device.index != torch._C._cuda_getDevice():
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name}: on {t.device}, which is not the current device (use torch.cuda.device)")
 
 
 def _thd(t: torch.Tensor, name: str) -> Tuple[int, int]:
     """(token stride, head stride) in elements of a bf16 [tokens, H, d] tensor, dim stride 1."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or not t.is_cuda or t.stride(2) != 1:
+    s = t.stride()
+    if t.dtype != torch.bfloat16 or len(s) != 3 or not t.is_cuda or s[2] != 1:
         raise ValueError(f"{name}: expected a CUDA bf16 [tokens, H, d] tensor with unit dim stride")
-    return t.stride(0), t.stride(1)
+    return s[0], s[1]
 
 
 # ------------------------------------------------------------------ C-named functions
@@ -379,13 +380,14 @@ def hsa_rope(x: torch.Tensor, out: torch.Tensor, rope: hsa_rope_args, flags: int
     """x, out: bf16, fp16 or fp32 [tokens, H, d] with unit dim stride; out may be x."""
     if x.dtype not in _TYPES or out.dtype != x.dtype:
         raise ValueError("hsa_rope: expected x and out of one type, bf16, fp16 or fp32")
-    if x.dim() != 3 or out.shape != x.shape or not x.is_cuda or out.device != x.device:
+    shape, s, o = x.shape, x.stride(), out.stride()
+    if len(shape) != 3 or out.shape != shape or not x.is_cuda or out.get_device() != x.get_device():
         raise ValueError("hsa_rope: expected CUDA tensors [tokens, H, d] of one shape")
-    if x.stride(2) != 1 or out.stride(2) != 1:
+    if s[2] != 1 or o[2] != 1:
         raise ValueError("hsa_rope: expected unit dim stride")
     _on_current(x, "x")
-    _check(_lib.hsa_rope(x.data_ptr(), out.data_ptr(), _TYPES[x.dtype], x.shape[0], x.shape[1], x.shape[2], x.stride(0),
-                         x.stride(1), out.stride(0), out.stride(1), C.byref(rope), int(flags), _stream()), "hsa_rope")
+    _check(_lib.hsa_rope(x.data_ptr(), out.data_ptr(), _TYPES[x.dtype], *shape, s[0], s[1], o[0], o[1], C.byref(rope),
+                         int(flags), _stream()), "hsa_rope")
 
 
 def hsa_kv8_query_sizes(cfg: hsa_kv8_config) -> hsa_kv8_sizes:
@@ -641,18 +643,18 @@ class RotaryPositions:
                                    trained_tokens, beta_fast, beta_slow)
         turns, amplitude = hsa_rope_table(self.cfg)
         self.turns = turns.to(device)
-        self.head_dim, self.device = head_dim, self.turns.device
+        self.head_dim, self.device, self._index = head_dim, self.turns.device, self.turns.get_device()
         self._args = (rot_dim, _LAYOUTS[layout], self.n_axes, axes, amplitude, self.turns.data_ptr())
 
     def args(self, positions: Optional[torch.Tensor], n_tokens: int) -> hsa_rope_args:
         """positions: int32 [tokens] or [axes, tokens] with unit token stride, or None: token i at position i."""
         stride = 0
         if positions is not None:
-            if positions.dtype != torch.int32 or positions.device != self.device:
+            if positions.dtype != torch.int32 or positions.get_device() != self._index:
                 raise ValueError("positions: expected int32 on the table's device")
             if positions.dim() == 1 and self.n_axes == 1:
                 positions = positions[None]
-            if positions.dim() != 2 or positions.shape != (self.n_axes, n_tokens) or (n_tokens > 1 and positions.stride(1) != 1):
+            if positions.shape != (self.n_axes, n_tokens) or (n_tokens > 1 and positions.stride(1) != 1):
                 raise ValueError(f"positions: expected [{self.n_axes}, {n_tokens}] with unit token stride")
             stride = positions.stride(0)
         return hsa_rope_args(*self._args, _ptr(positions), stride)
@@ -660,7 +662,7 @@ class RotaryPositions:
     def apply(self, x: torch.Tensor, positions: Optional[torch.Tensor] = None, transpose: bool = False,
               out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Rotates x [tokens, H, d]; transpose=True applies the transposed map, the gradient of the rotation."""
-        if x.dim() != 3 or x.shape[2] != self.head_dim or x.device != self.device:
+        if x.dim() != 3 or x.shape[2] != self.head_dim or x.get_device() != self._index:
             raise ValueError(f"x: expected [tokens, H, {self.head_dim}] on {self.device}")
         if out is None:
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -683,6 +685,7 @@ class KV8Cache:
         self.ctx = None
         dev = torch.device(device)
         self.device = torch.device("cuda", torch.cuda.current_device()) if dev.index is None and dev.type == "cuda" else dev
+        self._index = -1 if self.device.index is None else self.device.index  # as get_device() gives it
         self.num_heads, self.num_kv_heads, self.head_dim = num_heads, num_kv_heads, head_dim
         self.max_pages, self.max_blocks, self.max_batch, self.max_tokens = max_pages, max_blocks, max_batch, max_tokens
         self.cfg = hsa_kv8_config(num_heads, num_kv_heads, head_dim, PAGE_TOKENS, max_pages, max_blocks, max_batch,
@@ -715,17 +718,18 @@ class KV8Cache:
 
     def _rows(self, t: torch.Tensor, heads: int, counts: torch.Tensor, token_start: Optional[torch.Tensor],
               most: Optional[int], name: str) -> int:
-        if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or t.device != self.device:
+        shape, index = t.shape, self._index
+        if len(shape) != 3 or shape[1] != heads or shape[2] != self.head_dim or t.get_device() != index:
             raise ValueError(f"{name}: expected [tokens, {heads}, {self.head_dim}] on {self.device}")
         for x in (counts, token_start):
-            if x is not None and (x.dtype != torch.int32 or x.device != self.device or not x.is_contiguous() or x.dim() != 1):
+            if x is not None and (x.dtype != torch.int32 or x.get_device() != index or not x.is_contiguous() or x.dim() != 1):
                 raise ValueError("held, lengths, token_start: expected contiguous int32 vectors on the cache's device")
         if token_start is not None and token_start.numel() != counts.numel() + 1:
             raise ValueError("token_start: expected one entry more than there are sequences")
         _on_current(t, name)
         if most is not None:
             return int(most)
-        return t.shape[0] if token_start is not None else t.shape[0] // max(1, counts.numel())
+        return shape[0] if token_start is not None else shape[0] // max(1, counts.numel())
 
     def append(self, k: torch.Tensor, v: torch.Tensor, held: torch.Tensor, token_start: Optional[torch.Tensor] = None,
                max_new: Optional[int] = None, rope: Optional[RotaryPositions] = None,
@@ -734,9 +738,9 @@ class KV8Cache:
         int32 [batch + 1] where the sequences' rows differ in number, at most max_new to one.  Keys are rotated by
         `rope` at `positions` (default: their place in the sequence)."""
         most = self._rows(k, self.num_kv_heads, held, token_start, max_new, "k")
-        if v.device != self.device or v.shape != k.shape:
+        if v.get_device() != self._index or v.shape != k.shape:
             raise ValueError("k and v must share shape and device")
-        if rope is not None and (rope.device != self.device or rope.head_dim != self.head_dim):
+        if rope is not None and (rope._index != self._index or rope.head_dim != self.head_dim):
             raise ValueError("rope: of another device or head size")
         if rope is None and positions is not None:
             raise ValueError("positions without rope")
@@ -757,11 +761,11 @@ class KV8Cache:
             if tuple(sel_idx.shape[:-1]) != lists or tuple(sel_cnt.shape) != lists:
                 raise ValueError(f"sel_idx, sel_cnt: expected [{lists[0]}, {lists[1]}, n] and [{lists[0]}, {lists[1]}]")
             for x in (sel_idx, sel_cnt):
-                if x.dtype != torch.int32 or x.device != self.device or not x.is_contiguous():
+                if x.dtype != torch.int32 or x.get_device() != self._index or not x.is_contiguous():
                     raise ValueError("sel_idx, sel_cnt: expected contiguous int32 on the cache's device")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        elif out.shape != q.shape or out.device != q.device:
+        elif out.shape != q.shape or out.get_device() != self._index:
             raise ValueError("out: expected the shape and device of q")
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
         hsa_kv8_attend(self.ctx, q, lengths.numel(), token_start, most, lengths, causal, sel_idx, sel_cnt, out, lse)
