@@ -378,7 +378,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
             for (int term = 0; term < 2; ++term)
 #pragma unroll
               for (int kk = 0; kk < D / 32; ++kk)
-                mma_f8_lo(d, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, row_desc_hi<D>(), id_s, term + kk > 0);
+                mma_f8_lo(d, q + (term * kTile * D + kk * 32) / 16, k + kk * 2, row_desc_hi<D>(), row_desc_hi<D>(), id_s, term + kk > 0);
             tc_commit(&sm.s_full[b]);
             tc_commit(&sm.k_empty[st]);
           }
@@ -419,7 +419,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       }
       if (elect_one_sync()) tc_commit(&sm.done[t]);
       __syncwarp();
-      wait(&sm.done[t], 0);
+      if (mbar_poll(&sm.done[t], 0, 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
     } else {
       // ---- looks ahead for warps 1 and 2, who would otherwise poll three barriers for a page (each some 250 cycles beside busy
       // warps): arrives with the weights of a page where its values and the keys of the scores behind it are there.  Where the

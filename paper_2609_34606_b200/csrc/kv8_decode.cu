@@ -266,69 +266,74 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         mbar_poll(&sm.v_full[(n - i) % kStages], ((n - i) / kStages) & 1, 0);
       }
   } else if (warp == 1) {
-    // ---- first products
-    if (elect_one_sync()) {
-      constexpr uint32_t id = idesc_e4m3(128, N, 0, 0);
-      const uint64_t k0 = row_desc<D>(smem_u32(sm.k), 0), q0 = row_desc<D>(smem_u32(sm.q), 0);
-      uint32_t n = 0, items = 0, st = 0, round = 0;
-      while (ok && walk.next(a, w, sm.plan)) {
-        const uint32_t qb = items & 1;
-        if (!wait(&sm.q_full[qb], (items / 2) & 1)) break;
+    // ---- first products.  (The warps that issue products stay together and choose a lane at the last moment, so that the operands
+    // are in uniform registers.)
+    constexpr uint32_t id = idesc_e4m3(128, N, 0, 0);
+    const uint32_t k0 = row_desc_lo(smem_u32(sm.k)), q0 = row_desc_lo(smem_u32(sm.q)), tm = warp_uniform(tmem);
+    uint32_t n = 0, items = 0, st = 0, round = 0;
+    while (warp_uniform(walk.next(a, w, sm.plan))) {
+      const uint32_t qb = items & 1, steps = warp_uniform(walk.g.s1 - walk.g.s0);
+      wait(&sm.q_full[qb], (items / 2) & 1);
 #pragma unroll 1
-        for (int s = walk.g.s0; s < walk.g.s1; ++s, ++n) {
-          const uint32_t b = n & 1;
-          if (!wait(&sm.k_full[st], round & 1) || !wait(&sm.s_free[b], ((n / 2) & 1) ^ 1)) break;
-          tc_fence_after();
+      for (uint32_t s = 0; s < steps; ++s, ++n) {
+        const uint32_t b = n & 1, k = k0 + st * (Sh::kStage / 16), q = q0 + qb * (N * D / 16);
+        wait(&sm.k_full[st], round & 1);
+        wait(&sm.s_free[b], ((n / 2) & 1) ^ 1);
+        tc_fence_after();
+        if (elect_one_sync()) {
 #pragma unroll
           for (int kk = 0; kk < D / 32; ++kk)  // (descriptors count in 16 bytes)
-            mma_f8(tmem + Sh::kS + b * N, k0 + (st * Sh::kStage + kk * 32) / 16, q0 + (qb * (N * D) + kk * 32) / 16, id, kk > 0);
+            mma_f8_lo(tm + Sh::kS + b * N, k + kk * 2, q + kk * 2, row_desc_hi<D>(), row_desc_hi<D>(), id, kk > 0);
           tc_commit(&sm.s_full[b]);
-          if (s == walk.g.s1 - 1) tc_commit(&sm.q_free[qb]);
-          if (++st == kStages) {
-            st = 0;
-            ++round;
-          }
+          if (s + 1 == steps) tc_commit(&sm.q_free[qb]);
         }
-        ++items;
+        __syncwarp();
+        if (++st == kStages) {
+          st = 0;
+          ++round;
+        }
       }
-      tc_commit(&sm.done[0]);
-      mbar_poll(&sm.done[0], 0, 0);
+      ++items;
     }
+    if (elect_one_sync()) tc_commit(&sm.done[0]);
     __syncwarp();
+    if (mbar_poll(&sm.done[0], 0, 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
   } else if (warp == 3) {
-    // ---- second products, a page at a time
-    if (elect_one_sync()) {
-      constexpr uint32_t id = idesc_e4m3(128, N, 1, 0);
-      // (head_dim 64: the upper half of M reads what lies a page further, whatever that is; those lanes of the accumulator
-      // are not looked at)
-      const uint64_t v0 = row_desc<D>(smem_u32(sm.v), D == 128 ? 0 : Sh::kPage), p0 = row_desc<128>(smem_u32(sm.p), 0);
-      uint32_t n = 0, st = 0, round = 0;
-      while (ok && walk.next(a, w, sm.plan)) {
+    // ---- second products, a page at a time (of pages that are not there too: nobody looks at what they give)
+    constexpr uint32_t id = idesc_e4m3(128, N, 1, 0);
+    // (head_dim 64: the upper half of M reads what lies a page further, whatever that is; those lanes of the accumulator
+    // are not looked at)
+    const uint32_t v0 = row_desc_lo(smem_u32(sm.v)) | (D == 128 ? 0u : static_cast<uint32_t>(Sh::kPage >> 4) << 16),
+                   p0 = row_desc_lo(smem_u32(sm.p)), tm = warp_uniform(tmem);
+    uint32_t n = 0, st = 0, round = 0;
+    while (warp_uniform(walk.next(a, w, sm.plan))) {
+      const uint32_t steps = warp_uniform(walk.g.s1 - walk.g.s0);
 #pragma unroll 1
-        for (int s = walk.g.s0; s < walk.g.s1; ++s, ++n) {
-          const uint32_t b = n & 1;
-          if (!wait(&sm.p_full[b], (n / 2) & 1) || !wait(&sm.v_full[st], round & 1)) break;
-          tc_fence_after();
+      for (uint32_t s = 0; s < steps; ++s, ++n) {
+        const uint32_t b = n & 1, v = v0 + st * (Sh::kStage / 16), p = p0 + b * (N * 128 / 16);
+        wait(&sm.v_full[st], round & 1);
+        wait(&sm.p_full[b], (n / 2) & 1);
+        tc_fence_after();
+        if (elect_one_sync()) {
 #pragma unroll
           for (int pg = 0; pg < 2; ++pg)
-            if (sm.meta[st][pg].pos >= 0) {
 #pragma unroll
-              for (int half = 0; half < 2; ++half)  // 32 keys: rows of V, bytes of a row of P
-                mma_f8(tmem + Sh::kO + (b * 2 + pg) * N, v0 + (st * Sh::kStage + pg * Sh::kPage + half * 32 * D) / 16,
-                       p0 + (b * (N * 128) + pg * 64 + half * 32) / 16, id, half);
-            }
+            for (int half = 0; half < 2; ++half)  // 32 keys: rows of V, bytes of a row of P
+              mma_f8_lo(tm + Sh::kO + (b * 2 + pg) * N, v + (pg * Sh::kPage + half * 32 * D) / 16, p + (pg * 64 + half * 32) / 16,
+                        row_desc_hi<D>(), row_desc_hi<128>(), id, half);
           tc_commit(&sm.empty[st]);
           tc_commit(&sm.p_free[b]);
-          if (++st == kStages) {
-            st = 0;
-            ++round;
-          }
+        }
+        __syncwarp();
+        if (++st == kStages) {
+          st = 0;
+          ++round;
         }
       }
-      tc_commit(&sm.done[1]);
-      mbar_poll(&sm.done[1], 0, 0);
     }
+    if (elect_one_sync()) tc_commit(&sm.done[1]);
     __syncwarp();
+    if (mbar_poll(&sm.done[1], 0, 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
   } else if (warp == 2) {
     // ---- rows of Q, an item ahead: a thread takes 8 dims of a row
     uint32_t items = 0;

@@ -57,16 +57,6 @@ __device__ __forceinline__ void tc_commit_if(uint64_t* bar, bool yes) {
 __device__ __forceinline__ void mbar_expect_tx_only(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n"
-      "}\n" ::"r"(d_tmem),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
 // kind::f8f6f4, e4m3 operands (format 0), fp32 accumulator; bits as idesc_bf16_f32
 __host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N, uint32_t a_mn, uint32_t b_mn) {
   return (1u << 4) | (a_mn << 15) | (b_mn << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
@@ -75,30 +65,25 @@ __host__ __device__ constexpr uint32_t idesc_e4m3(uint32_t M, uint32_t N, uint32
 __host__ __device__ constexpr uint32_t idesc_fp16(uint32_t M, uint32_t N, uint32_t a_mn, uint32_t b_mn) { return idesc_e4m3(M, N, a_mn, b_mn); }
 // lane 0's value; what comes of it is the same for the whole warp, which the compiler knows
 __device__ __forceinline__ uint32_t warp_uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
-// Rows of D bytes in the swizzle that spans a row (128 bytes: layout 2, 64 bytes: layout 4); eight rows are 8 * D bytes.
-template <int D>
-__device__ __forceinline__ uint64_t row_desc(uint32_t addr, uint32_t lbo) {
-  return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(lbo >> 4) << 16 |
-         static_cast<uint64_t>((8 * D) >> 4) << 32 | static_cast<uint64_t>(1) << 46 |
-         static_cast<uint64_t>(D == 128 ? 2 : 4) << 61;
-}
-// The two words of it, without a leading offset.
+// Descriptors of rows of D bytes in the swizzle that spans a row (128 bytes: layout 2, 64 bytes: layout 4); eight rows are 8 * D
+// bytes.  The low word is without a leading offset.
 __device__ __forceinline__ uint32_t row_desc_lo(uint32_t addr) { return (addr & 0x3FFFFu) >> 4; }
 template <int D>
 __host__ __device__ constexpr uint32_t row_desc_hi() {
   return ((8 * D) >> 4) | 1u << 14 | (D == 128 ? 2u : 4u) << 29;
 }
-__device__ __forceinline__ void mma_f8_lo(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_f8_lo(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t a_hi, uint32_t b_hi, uint32_t idesc,
+                                          uint32_t accumulate) {
   asm volatile(
       "{\n"
       ".reg .pred p;\n"
       ".reg .b64 da, db;\n"
-      "setp.ne.b32 p, %5, 0;\n"
+      "setp.ne.b32 p, %6, 0;\n"
       "mov.b64 da, {%1, %3};\n"
-      "mov.b64 db, {%2, %3};\n"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %4, p;\n"
+      "mov.b64 db, {%2, %4};\n"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], da, db, %5, p;\n"
       "}\n" ::"r"(d_tmem),
-      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate)
+      "r"(a_lo), "r"(b_lo), "r"(a_hi), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // Byte of (row, byte in the row) in such a tile.
