@@ -46,12 +46,9 @@ __device__ __forceinline__ uint32_t mbar_poll(uint64_t* bar, uint32_t parity, ui
       : "memory");
   return after;
 }
-// arrivals and commits by some threads or sometimes, without a branch
+// an arrival by some threads or sometimes, without a branch
 __device__ __forceinline__ void mbar_arrive_if(uint64_t* bar, bool yes) {
   asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p mbarrier.arrive.shared::cta.b64 _, [%0];\n}\n" ::"r"(smem_u32(bar)), "r"(static_cast<uint32_t>(yes)) : "memory");
-}
-__device__ __forceinline__ void tc_commit_if(uint64_t* bar, bool yes) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar)), "r"(static_cast<uint32_t>(yes)) : "memory");
 }
 // the bytes alone: the arrival comes later
 __device__ __forceinline__ void mbar_expect_tx_only(uint64_t* bar, uint32_t bytes) {

@@ -625,3 +625,64 @@ def test_rollout_positions_append_select_attend(cuda_device):
             c.take_gpu_state()
             c.attend([1], True)
     assert c.cache.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 17])
+def test_attend_more_sequences_than_a_plan_lists(cuda_device, n):
+    """5600 (sequence, head) pairs: every CTA has more of them than its list of runs holds, for one query and for many."""
+    rng = np.random.default_rng(n)
+    lengths = [int(x) for x in rng.integers(n, 140, 700)]
+    lengths[5] = lengths[699] = n
+    c = Case(cuda_device, 8, 8, 64, lengths, seed=16, max_tokens=sum(lengths))
+    c.append(lengths, twin=False)
+    c.take_gpu_state()
+    c.attend([n] * 700, True)
+    c.attend([n if i % 3 else 0 for i in range(700)], False)
+    assert c.cache.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("counts", [[1], [30], [150]])
+@pytest.mark.parametrize("far", [-120.0, 120.0])
+def test_value_scales_far_apart(cuda_device, d, counts, far):
+    """Pages whose values differ by 2^80: a page of huge values that nothing points at (`far` < 0) leaves the others their
+    precision, and one that everything points at gives the result whatever the others hold."""
+    c = Case(cuda_device, 2, 2, d, [256], seed=17)
+    k, v = c.randn(256, 2, d), c.randn(256, 2, d)
+    k[:, :, 0] = 0
+    k[64:128, :, 0] = far * math.log(2) * math.sqrt(d)      # with a query of 1 there: weights of 2^far
+    v[64:128] *= 2.0 ** 45
+    v[128:192] *= 2.0 ** -35
+    q = c.randn(sum(counts), 2, d)
+    q[:, :, 0] = 1
+    c.append([256], k=k, v=v)
+    c.take_gpu_state()
+    _, got, lse = c.attend(counts, False, q=q)
+    ref = O.attend([q.double().numpy()], c.state, c.table.numpy(), [256], False)[0]
+    # the pages that weigh: half a step of bf16 for the result and 2^-8 for the weights; scores as in assert_attention
+    score = 2.0 ** -16 * float(q.abs().max()) * float(k.double().abs().sum(-1).max()) / math.sqrt(d) + 2.0 ** -20
+    if far < 0:
+        bound = 2.0 ** -8 * np.abs(ref[0]) + (2.0 ** -8 * 1.02 + 2 * score) * ref[2] + 2.0 ** -20 * 256 * 6
+        assert (np.abs(got.double().cpu().numpy() - ref[0]) <= bound).all()
+    else:
+        bound = 2.0 ** -8 * np.abs(ref[0]) + (2.0 ** -8 * 1.02 + 2 * score) * ref[2] + 2.0 ** -20 * ref[3]
+        assert (np.abs(got.double().cpu().numpy() - ref[0]) <= bound).all()
+    assert c.cache.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [[100], [20, 3], [128, 128]])
+def test_a_tile_of_rows_shared_by_both_halves_of_the_kernel(cuda_device, counts):
+    """Items of at most 128 rows, whose pages two groups of warps take in turn: histories of one page, of two, of an odd
+    number, and long ones that are split over the device."""
+    for lengths in ([128 + 0, 128], [129, 200], [64 * 7, 64 * 9 + 1], [9000, 6001]):
+        lengths = lengths[:len(counts)]
+        for d, Hq, Hkv in ((128, 2, 2), (64, 5, 1) if max(counts) <= 20 else (64, 1, 1)):
+            c = Case(cuda_device, Hq, Hkv, d, lengths, seed=18, max_tokens=16000)
+            c.append(lengths, twin=False)
+            c.take_gpu_state()
+            c.attend(counts, True)
+            c.attend(counts, False)
+            assert c.cache.device_status() == 0
