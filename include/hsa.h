@@ -489,8 +489,10 @@ int hsa_kv8_append(hsa_kv8* ctx, const void* k, const void* v, int32_t n_tokens,
  *   sel_cnt_dev      device int32[batch][num_kv_heads] their lengths (clamped to 0..max_topk)
  *   lse_dev          device fp32 [n_tokens][num_heads] receiving ln sum_j exp(scale q . k_j), or NULL
  * A block that a list names twice counts twice.  A query that sees nothing gets zeros and an lse of -inf.  Rows of
- * out that belong to no sequence are left as they were.  What the result is made of: products exact, sums in fp32,
- * softmax weights rounded to 8 significant bits or more (see the kernels).  Sequences that do not fit (as above,
+ * out that belong to no sequence are left as they were, and so are those of lse.  What the result is made of: queries
+ * exact, but for values below 2^-10 of their row's largest, which may be off by 2^-18 of that; products exact, sums in
+ * fp32; softmax weights (times their page's value scale, where a call has more than 16 query rows of a key head) rounded to
+ * 8 significant bits or to 2^-21 of the largest one.  Sequences that do not fit (as above,
  * lengths < 0 or past max_blocks) are left out, list entries outside [0, max_blocks) and pages outside the pools count
  * as not seen, both with HSA_ERR_DEVICE_BOUNDS; list entries behind the length see nothing. */
 int hsa_kv8_attend(hsa_kv8* ctx, const void* q, int32_t n_tokens, int32_t batch, int64_t tok_stride,

@@ -15,14 +15,21 @@
 //
 // An item has 256 rows, two tiles of 128, so that every page that is read and turned into fp16 serves both.  A tile's S has
 // two buffers of a page's 64 keys: the products of a page run while the softmax is at the page before it.  (With one buffer of
-// 128 keys products are a fifth faster, but products and softmax of a tile wait for each other: 1543 us instead of XXX for 4680
-// queries, 46,800 tokens, 12 heads.)  An item of 128 rows or fewer gives both tiles to the same rows: they take its pages in
-// turn and are brought together at its end.
+// 128 keys products take 2048 cycles for two tiles and two pages instead of 2500, but products and softmax of a tile wait for each
+// other: 1543 us instead of 1237 for the chunk below.)  An item of 128 rows or fewer gives both tiles to the same rows: they take its
+// pages in turn and are brought together at its end.
 //
 // Warps: 0 loads pages, 1 and 2 issue the products of a tile each, 3 looks ahead for them, 4 - 7 turn values into fp16, 8 - 11
 // and 12 - 15 are the softmax of a tile each, a row to a thread, whose query they also bring into its two terms.
 // The warps that issue products stay together and choose a lane for it at the last moment: so their operands are in uniform
 // registers.  A loop of one lane alone takes some 75 cycles to issue a product, beside busy warps, more than the product's 64.
+//
+// Measured: 4680 queries, 46,800 tokens, 12 heads of 128: 1160 us in a short run (1160 TFLOP/s), 1338 in a long one, at the
+// board's 1 kW (1005 TFLOP/s; a library product of bf16 alone holds 1373).  A page takes 1750 to 1900 cycles for both tiles: its
+// products 1280, its exponentials, of two warps on a special function unit at the same time, 1024.  What was tried and did not
+// help: turns at the exponentials (1192 us), an eighth or a quarter of them as polynomials (1185, 1196), half a row to a thread and
+// twice the warps (1400 against 1319), the next page's scores asked for early (1264 against 1237).
+// Heads of 64 have half the products and the same exponentials: the softmax bounds them, and 10,000 cycles an item at its ends.
 // Tensor memory: four S (P, packed fp16, over their first halves), O of both tiles.
 #include "kv8.cuh"
 #include "kv8_mma.cuh"

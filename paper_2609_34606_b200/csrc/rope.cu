@@ -3,6 +3,8 @@
 // What it needs: every value read once and written once; the arithmetic (three operations a value, a sine and a cosine a
 // pair and token) hides behind that if the sines are not worked out again for every head.  So a thread owns a few pairs
 // of a token and walks over heads with them.
+// Measured: 20,011 tokens x 8 heads of 128 in fp32 26.4 us (6.2 TB/s; a plain copy 6.54), 20,011 x 12 in bf16 27.4 us (4.5 TB/s:
+// eight sines to 32 bytes of a row), 4680 x 12 7.0 us, one token 3 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
