@@ -378,7 +378,8 @@ def hsa_rope_table(cfg: hsa_rope_config) -> Tuple[torch.Tensor, float]:
 
 def hsa_rope(x: torch.Tensor, out: torch.Tensor, rope: hsa_rope_args, flags: int = 0) -> None:
     """x, out: bf16, fp16 or fp32 [tokens, H, d] with unit dim stride; out may be x."""
-    if x.dtype not in _TYPES or out.dtype != x.dtype:
+    code = _TYPES.get(x.dtype)
+    if code is None or out.dtype != x.dtype:
         raise ValueError("hsa_rope: expected x and out of one type, bf16, fp16 or fp32")
     shape, s, o = x.shape, x.stride(), out.stride()
     if len(shape) != 3 or out.shape != shape or not x.is_cuda or out.get_device() != x.get_device():
@@ -386,7 +387,7 @@ def hsa_rope(x: torch.Tensor, out: torch.Tensor, rope: hsa_rope_args, flags: int
     if s[2] != 1 or o[2] != 1:
         raise ValueError("hsa_rope: expected unit dim stride")
     _on_current(x, "x")
-    _check(_lib.hsa_rope(x.data_ptr(), out.data_ptr(), _TYPES[x.dtype], *shape, s[0], s[1], o[0], o[1], C.byref(rope),
+    _check(_lib.hsa_rope(x.data_ptr(), out.data_ptr(), code, *shape, s[0], s[1], o[0], o[1], C.byref(rope),
                          int(flags), _stream()), "hsa_rope")
 
 
@@ -665,7 +666,7 @@ class RotaryPositions:
         if x.dim() != 3 or x.shape[2] != self.head_dim or x.get_device() != self._index:
             raise ValueError(f"x: expected [tokens, H, {self.head_dim}] on {self.device}")
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            out = x.new_empty(x.shape)
         hsa_rope(x, out, self.args(positions, x.shape[0]), HSA_ROPE_TRANSPOSE if transpose else 0)
         return out
 
@@ -764,10 +765,11 @@ class KV8Cache:
                 if x.dtype != torch.int32 or x.get_device() != self._index or not x.is_contiguous():
                     raise ValueError("sel_idx, sel_cnt: expected contiguous int32 on the cache's device")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         elif out.shape != q.shape or out.get_device() != self._index:
             raise ValueError("out: expected the shape and device of q")
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if with_lse else None
+        # (new_empty: 1.9 us on the host; torch.empty of a slice of the shape on a device: 3.4)
+        lse = q.new_empty((q.shape[0], self.num_heads), dtype=torch.float32) if with_lse else None
         hsa_kv8_attend(self.ctx, q, lengths.numel(), token_start, most, lengths, causal, sel_idx, sel_cnt, out, lse)
         return (out, lse) if with_lse else out
 
