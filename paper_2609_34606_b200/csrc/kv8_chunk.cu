@@ -111,11 +111,12 @@ __device__ __forceinline__ uint32_t fp16_of(uint32_t two) {
   asm("{\n.reg .b16 lo, hi;\nmov.b32 {lo, hi}, %1;\ncvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(d) : "r"(two));
   return d;
 }
-// 32 rows of the queries (row r at q_in + `from` of lane r, if it is in `there`) as two e4m3 terms into the rows from `first` on of
-// the tiles at q and behind it.  Lane r gets what its row has been divided by.  Lanes next to each other read a row together.
+// Rows lo .. hi of 32 rows of the queries (row r at q_in + `from` of lane r, if it is in `there`) as two e4m3 terms into the rows from
+// `first` on of the tiles at q and behind it.  Lane r gets what its row has been divided by.  Lanes next to each other read a row together.
 // (Short code: it runs once an item, and has to come from far each time.)
 template <int D>
-__device__ __forceinline__ float two_terms(const __nv_bfloat16* q_in, int64_t from, uint32_t there, uint8_t* q, int first, int lane) {
+__device__ __forceinline__ float two_terms(const __nv_bfloat16* q_in, int64_t from, uint32_t there, uint8_t* q, int first, int lane,
+                                          int lo, int hi) {
   constexpr int C = D / 8, R = 32 / C, kAtOnce = 4;  // vectors of a row, rows at a time, loads in flight (and as many behind them)
   const int e = lane % C, k0 = lane / C;
   float mine = 1.f;
@@ -128,9 +129,9 @@ __device__ __forceinline__ float two_terms(const __nv_bfloat16* q_in, int64_t fr
       next[i] = there >> k & 1 ? __ldg(reinterpret_cast<const uint4*>(q_in + at) + e) : make_uint4(0, 0, 0, 0);
     }
   };
-  load(0);
+  load(lo);
 #pragma unroll 1
-  for (int base = 0; base < 32; base += R * kAtOnce) {
+  for (int base = lo; base < hi; base += R * kAtOnce) {
     uint32_t top[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
@@ -159,7 +160,7 @@ __device__ __forceinline__ float two_terms(const __nv_bfloat16* q_in, int64_t fr
       const uint32_t* x = &in[i].x;
       const int k = base + i * R + k0, ex = max(static_cast<int>(top[i] >> 7) - 127, -100) - 7;  // (rows of zeros: any will do)
       const float up = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
-      uint32_t hi[4], lo[4];
+      uint32_t big[4], small[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         // (fp16 has the 8 bits of these values, down to 2^-14, far below the last one of the second term)
@@ -179,12 +180,12 @@ __device__ __forceinline__ float two_terms(const __nv_bfloat16* q_in, int64_t fr
             "cvt.u32.u16 %0, h;\n"
             "cvt.u32.u16 %1, l;\n"
             "}\n"
-            : "=r"(hi[j]), "=r"(lo[j])
+            : "=r"(big[j]), "=r"(small[j])
             : "r"(x[j]), "f"(up));
       }
       uint8_t* at = q + swizzled<D>(first + k, e * 8);
-      *reinterpret_cast<uint2*>(at) = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-      *reinterpret_cast<uint2*>(at + kTile * D) = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
+      *reinterpret_cast<uint2*>(at) = make_uint2(big[0] | big[1] << 16, big[2] | big[3] << 16);
+      *reinterpret_cast<uint2*>(at + kTile * D) = make_uint2(small[0] | small[1] << 16, small[2] | small[3] << 16);
       // rows base + i R .. + R are in the groups of C lanes
       const uint32_t of = __shfl_sync(0xffffffffu, 127 + ex, (lane % R) * C);
       if (lane / R == base / R + i) mine = __uint_as_float(of << 23);
@@ -497,13 +498,14 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       const bool mine = row < it.rows;
       const int at = it.row0 + min(row, it.rows - 1), head = it.h * a.group + at % a.group;
       const int64_t tok = it.first + at / a.group;
-      // the row into its two terms (nobody reads what was there: this tile's scores of the last item have been seen, and with this
-      // barrier all its rows have been written out)
-      tile_sync(t);
-      if (!same || t == 0) {
-        sm.qscale[row] = a.scale_log2 * two_terms<D>(a.q, tok * a.ts + head * a.hs, __ballot_sync(0xffffffffu, mine), sm.q[t][0], r - lane, lane);
-        fence_proxy_async_smem();
-      }
+      // The rows into their two terms; of shared ones each tile's warps do half.  (Nobody reads what was there: the scores of the
+      // last item have been seen, and with this barrier all its rows have been written out.)
+      if (same) tiles_sync();
+      else tile_sync(t);
+      const int lo = same ? t * 16 : 0, hi = same ? lo + 16 : 32;
+      const float e = two_terms<D>(a.q, tok * a.ts + head * a.hs, __ballot_sync(0xffffffffu, mine), sm.q[same ? 0 : t][0], r - lane, lane, lo, hi);
+      if (lane >= lo && lane < hi) sm.qscale[row] = e * a.scale_log2;
+      fence_proxy_async_smem();
       __syncwarp();
       mbar_arrive_if(&sm.q_full, lane == 0);
       if (same) {
