@@ -140,14 +140,15 @@ __global__ void __launch_bounds__(kThreads<D>, D == 128 ? 2 : 4) kv8_append_kern
   constexpr bool swaps = MODE == kHalf || MODE == kHalfOdd;  // partners are in other threads' vectors
   const auto is_new = [&](int i) { return row0 + i * R >= r0 && row0 + i * R < r1; };
   uint4 kx[I], vx[I];
+  const int64_t base = (src0 + row0) * a.ts + u * 8, step = R * a.ts;
   const auto load = [&](int h) {
-    const int64_t at = src0 * a.ts + h * a.hs + u * 8;
+    const int64_t at = base + h * a.hs;
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       kx[i] = vx[i] = make_uint4(0, 0, 0, 0);
       if (is_new(i)) {
-        kx[i] = __ldg(reinterpret_cast<const uint4*>(a.k + at + (row0 + i * R) * a.ts));
-        vx[i] = __ldg(reinterpret_cast<const uint4*>(a.v + at + (row0 + i * R) * a.ts));
+        kx[i] = __ldg(reinterpret_cast<const uint4*>(a.k + at + i * step));
+        vx[i] = __ldg(reinterpret_cast<const uint4*>(a.v + at + i * step));
       }
     }
   };
@@ -293,32 +294,33 @@ __global__ void __launch_bounds__(kThreads<D>, D == 128 ? 2 : 4) kv8_append_kern
       a.k_scale[ph] = scale_k;
       a.v_scale[ph] = scale_v;
     }
-    const int64_t to = ph * (kBlock * D) + u * 8;
+    const int64_t to = ph * (kBlock * D) + row0 * D + u * 8;
     float sum[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] = 0.f;
 #pragma unroll
     for (int i = 0; i < I; ++i) {
       if (!is_new(i) && r0 > 0) continue;  // (rows behind the last one of a block that begins here: zeros)
-      const int64_t at = to + (row0 + i * R) * D;
       float y[8];
       unpack(v[i], y);
-      *reinterpret_cast<uint2*>(a.k_pool + at) = codes(x[i], inv_k);
-      *reinterpret_cast<uint2*>(a.v_pool + at) = codes(y, inv_v);
+      *reinterpret_cast<uint2*>(a.k_pool + to + i * (R * D)) = codes(x[i], inv_k);
+      *reinterpret_cast<uint2*>(a.v_pool + to + i * (R * D)) = codes(y, inv_v);
+      if (sums) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] += x[i][j];
+        for (int j = 0; j < 8; ++j) sum[j] += x[i][j];
+      }
     }
     if (r0 > 0 && (scale_k > old_k || scale_v > old_v || sums)) {
       // rows of earlier calls, and those behind the last: their codes follow a scale that has grown
 #pragma unroll 1
       for (int job = 0; job < 2 * I; ++job) {
         const bool is_k = job < I;
-        const int r = row0 + (is_k ? job : job - I) * R;
+        const int i = is_k ? job : job - I, r = row0 + i * R;
         const float old_scale = is_k ? old_k : old_v, scale = is_k ? scale_k : scale_v;
         const bool summed = is_k && sums && r < r0;
         if ((r >= r0 && r < r1) || !(scale > old_scale || summed)) continue;
         const float shrink = old_scale * (is_k ? inv_k : inv_v);
-        uint2* at = reinterpret_cast<uint2*>((is_k ? a.k_pool : a.v_pool) + to + r * D);
+        uint2* at = reinterpret_cast<uint2*>((is_k ? a.k_pool : a.v_pool) + to + i * (R * D));
         const uint2 c = *at;
         float y[8];
         values(c, y);
