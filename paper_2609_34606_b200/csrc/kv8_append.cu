@@ -9,8 +9,8 @@
 // one barrier a head does for the maxima of keys and values, the partners of the next head's half layout, and the sums of the last
 // head's keys.  (With four barriers a head and nothing in flight across them 31 us instead of 18 for 4680 tokens, 12 heads of 128.)
 // Measured: 4680 tokens, 12 heads of 128 with positions and sums, 43 MB: 18 us (2.5 TB/s: two CTAs to an SM, a start and three heads
-// each); 30,000 tokens of 8 heads without positions 36 us (5.1 TB/s), with them 59 (the rotation's instructions: the schedulers
-// issue two cycles of three); ragged prompts, heads of 64, 270 MB: 62 us (4.4 TB/s); a token of 48 sequences 5.9 us, of which the
+// each); 30,000 tokens of 8 heads without positions 36 us (5.1 TB/s), with them 60 (the rotation's instructions: the schedulers
+// issue two cycles of three); ragged prompts, heads of 64, 270 MB: 52 us (5.2 TB/s); a token of 48 sequences 5.9 us, of which the
 // launch is 3 and the rest loads that wait for one another.
 #include <cuda_fp8.h>
 
@@ -155,12 +155,13 @@ __global__ void __launch_bounds__(kThreads<D>, D == 128 ? 2 : 4) kv8_append_kern
   load(h0);
   const int page = __ldg(a.table + static_cast<int64_t>(b) * a.max_blocks + blk);
   if constexpr (MODE != kPlain) {
-    // A row's pairs side by side in threads: one position, consecutive frequencies.
-    for (int i = tid; i < (r1 - r0) * a.rope.half; i += kThreads<D>) {
-      const int r = r0 + i / a.rope.half, p = i % a.rope.half;
-      const float2 cs = rope_cos_sin(a.rope, p, src0 + r, static_cast<int32_t>(t0 + r));
-      sm.cs[r][cos_at<D, MODE>(p)] = cs.x;
-      sm.cs[r][sin_at<D, MODE>(p)] = cs.y;
+    // A row to a warp, its pairs side by side in lanes: one position, consecutive frequencies.
+    for (int r = r0 + warp; r < r1; r += kThreads<D> / 32) {
+      for (int p = lane; p < a.rope.half; p += 32) {
+        const float2 cs = rope_cos_sin(a.rope, p, src0 + r, static_cast<int32_t>(t0 + r));
+        sm.cs[r][cos_at<D, MODE>(p)] = cs.x;
+        sm.cs[r][sin_at<D, MODE>(p)] = cs.y;
+      }
     }
     if constexpr (swaps) {
 #pragma unroll
@@ -374,12 +375,14 @@ cudaError_t launch_kv8_append(const Kv8AppendArgs& args, int D, int nsm, cudaStr
   Kv8AppendArgs a = args;
   a.blocks_per_seq = (a.rows.max_rows + 2 * kBlock - 2) / kBlock;
   const int64_t blocks = static_cast<int64_t>(a.rows.batch) * a.blocks_per_seq;
-  // Heads of a CTA: as many as leave two CTAs to an SM, at most 16: with positions they share the sines, and all share a CTA's start.
-  const int64_t heads = blocks * a.H / (2 * static_cast<int64_t>(nsm));
-  a.heads = static_cast<int>(heads < 1 ? 1 : heads > 16 ? 16 : heads);
-  if (a.heads > a.H) a.heads = a.H;
+  // Heads of a CTA: as many as leave two CTAs to an SM, at most 6, in even shares: with positions they share the sines, and all share a
+  // CTA's start.  (At most 16: ragged prompts of 16 heads of 64 61 us instead of 52, for want of CTAs to even out the last ones.)
+  int64_t heads = blocks * a.H / (2 * static_cast<int64_t>(nsm));
+  heads = heads < 1 ? 1 : heads > 6 ? 6 : heads > a.H ? a.H : heads;
+  const int groups = static_cast<int>((a.H + heads - 1) / heads);
+  a.heads = (a.H + groups - 1) / groups;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks), (a.H + a.heads - 1) / a.heads);
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks), groups);
   cfg.blockDim = dim3(D == 128 ? kThreads<128> : kThreads<64>);
   cfg.dynamicSmemBytes = D == 128 ? sizeof(AppendSmem<128>) : sizeof(AppendSmem<64>);
   cfg.stream = st;
