@@ -50,17 +50,17 @@ struct ChunkSmem {
   static constexpr int kKStages = D == 128 ? 6 : 12, kVStages = 4, kBStages = 4;  // pages
   union {
     uint8_t q[2][2][kTile * D];        // [tile][term]
-    float other[D][kTile];             // O of the second tile, where both have the same rows
+    float other[D][kTile];             // where both tiles have the same rows: what each gives the other of O
   };
   uint8_t k[kKStages][kPage];
   uint8_t vc[kVStages][kPage];         // codes
   uint8_t vb[kBStages][kPage * 2];     // fp16, [64 dims][key][64 dims]
   float qscale[2 * kTile];
-  float other_ref[kTile], other_sum[kTile];
+  float other_ref[2][kTile], other_sum[2][kTile];
   PageMeta meta[kMetas];
   int last[2];
   uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[kBStages], vb_empty[kBStages];
-  uint64_t s_full[4], p_full[4], pv_done[4], q_full, other_full, done[2];
+  uint64_t s_full[4], p_full[4], pv_done[4], q_full, done[2];
   uint32_t tmem;
   Kv8Plan plan;
 };
@@ -203,13 +203,14 @@ __device__ __forceinline__ float* part_of(const Kv8Work& w, int64_t slot, int ti
   return w.parts + slot * w.slot_floats + tile * (kTile * (D + 2));
 }
 
-// A row of an item that is shared by CTAs, from all their parts.
+// Dims d0 .. d1 of a row of an item that is shared by CTAs, from all their parts.
 template <int D>
-__device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w, const Kv8Segment& g, int t, int r, __nv_bfloat16* out, int64_t lse_at) {
+__device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w, const Kv8Segment& g, int t, int r, int d0, int d1, __nv_bfloat16* out,
+                                        int64_t lse_at) {
   float m = kNone, l = 0.f;
   for (int j = g.first_cta; j <= g.last_cta; ++j) m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
 #pragma unroll 1
-  for (int c = 0; c < D; c += 32) {
+  for (int c = d0; c < d1; c += 32) {
     float4 o[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -235,7 +236,7 @@ __device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w
           make_uint4(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv),
                      pack_bf16(o[k + 1].x * inv, o[k + 1].y * inv), pack_bf16(o[k + 1].z * inv, o[k + 1].w * inv));
   }
-  if (a.lse) a.lse[lse_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  if (a.lse && d0 == 0) a.lse[lse_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }
 
 template <int D>
@@ -265,7 +266,6 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       mbar_init(&sm.pv_done[i], 1);
     }
     mbar_init(&sm.q_full, 8);
-    mbar_init(&sm.other_full, 4);
     mbar_init(&sm.done[0], 1);
     mbar_init(&sm.done[1], 1);
     fence_mbar_init();
@@ -488,7 +488,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     const int t = (warp - 8) / 4, r = (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t col_o = tmem + lanes + kColO + t * 128;
-    uint32_t items = 0, n = 0, kn = 0, merges = 0;  // items, units of this tile, pages before the item's first
+    uint32_t items = 0, n = 0, kn = 0;  // items, units of this tile, pages before the item's first
     while (walk.next(a, w, sm.plan)) {
       const Kv8Item& it = walk.g.it;
       const bool same = shared_rows(it);
@@ -582,31 +582,26 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       tc_fence_after();
       ++items;
       if (same) tiles_sync();  // (`other` lies where the queries are: both tiles have all their scores)
+      // Of shared rows each tile brings half of the dims to their end: it gives its sums of the other half.
       float down = 1.f, take = 0.f;  // what this tile's O counts, and the other's
+      const int d0 = same ? t * (D / 2) : 0, d1 = same ? d0 + D / 2 : D;
       if (same) {
-        if (t == 1) {
+        const int give = D / 2 - d0;
 #pragma unroll 1
-          for (int i = 0; i < D; i += 32) {
-            uint32_t o[32];
-            tmem_ld32(col_o + i, o);
-            tc_wait_ld();
+        for (int i = give; i < give + D / 2; i += 32) {
+          uint32_t o[32];
+          tmem_ld32(col_o + i, o);
+          tc_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) sm.other[i + j][r] = __uint_as_float(o[j]);
-          }
-          sm.other_ref[r] = ref;
-          sm.other_sum[r] = l;
-          __syncwarp();
-          mbar_arrive_if(&sm.other_full, lane == 0);
-          tiles_sync();  // (`other` has been read)
-          continue;
+          for (int j = 0; j < 32; ++j) sm.other[i + j][r] = __uint_as_float(o[j]);
         }
-        wait(&sm.other_full, merges & 1);
-        __syncwarp();
-        ++merges;
-        const float m = sm.other_ref[r], to = fmaxf(ref, m);
-        down = ex2(ref - to);
-        take = ex2(m - to);
-        l = fmaf(sm.other_sum[r], take, l * down);
+        sm.other_ref[t][r] = ref;
+        sm.other_sum[t][r] = l;
+        tiles_sync();
+        const float r0 = sm.other_ref[0][r], r1 = sm.other_ref[1][r], to = fmaxf(r0, r1), f0 = ex2(r0 - to), f1 = ex2(r1 - to);
+        down = t == 0 ? f0 : f1;
+        take = t == 0 ? f1 : f0;
+        l = fmaf(sm.other_sum[1][r], f1, sm.other_sum[0][r] * f0);
         ref = to;
       }
       // Is the item shared with other CTAs, then the last one of them joins the parts, in the order of the CTAs whoever that is, its
@@ -651,7 +646,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       // other (`other` leaves no place for that).
       uint8_t* rows = sm.q[t][0] + (warp & 3) * (32 * D * 2);
 #pragma unroll 1
-      for (int i = 0; i < D; i += 32) {
+      for (int i = d0; i < d1; i += 32) {
         uint32_t o[32];
         tmem_ld32(col_o + i, o);
         tc_wait_ld();
@@ -718,7 +713,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       }
       if (real) {
         if (writes) {
-          if (a.lse) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
+          if (a.lse && d0 == 0) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
         } else {
           __stcg(part + kTile * D + r, ref);
           __stcg(part + kTile * D + kTile + r, l);
@@ -738,7 +733,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           sm.last[t] = last;
         }
         tile_sync(t);
-        if (sm.last[t] && real) join_parts<D>(a, w, g, t, r, out, tok * a.Hq + head);  // (the last of the others came meanwhile)
+        if (sm.last[t] && real) join_parts<D>(a, w, g, t, r, d0, d1, out, tok * a.Hq + head);  // (the last of the others came meanwhile)
       }
     }
   }
