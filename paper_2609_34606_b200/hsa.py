@@ -405,22 +405,19 @@ def hsa_kv8_create(cfg: hsa_kv8_config, bufs: hsa_kv8_buffers) -> int:
 
 def hsa_kv8_append(ctx: int, k: torch.Tensor, v: torch.Tensor, batch: int, token_start: Optional[torch.Tensor],
                    max_new: int, held: torch.Tensor, rope: Optional[hsa_rope_args] = None) -> None:
-    ts, hs = _thd(k, "k")
-    if _thd(v, "v") != (ts, hs) or v.shape != k.shape:
+    strides, shape = _thd(k, "k"), k.shape
+    if _thd(v, "v") != strides or v.shape != shape:
         raise ValueError("k and v must share shape and strides")
-    _check(_lib.hsa_kv8_append(ctx, k.data_ptr(), v.data_ptr(), k.shape[0], int(batch), ts, hs, _ptr(token_start),
-                               int(max_new), held.data_ptr(), C.byref(rope) if rope is not None else None, _stream()),
-           "hsa_kv8_append")
+    _check(_lib.hsa_kv8_append(ctx, k.data_ptr(), v.data_ptr(), shape[0], batch, *strides, _ptr(token_start), max_new,
+                               held.data_ptr(), None if rope is None else C.byref(rope), _stream()), "hsa_kv8_append")
 
 
 def hsa_kv8_attend(ctx: int, q: torch.Tensor, batch: int, token_start: Optional[torch.Tensor], max_q: int,
                    lengths: torch.Tensor, causal: bool, sel_idx: Optional[torch.Tensor], sel_cnt: Optional[torch.Tensor],
                    out: torch.Tensor, lse: Optional[torch.Tensor] = None) -> None:
-    ts, hs = _thd(q, "q")
-    ots, ohs = _thd(out, "out")
-    _check(_lib.hsa_kv8_attend(ctx, q.data_ptr(), q.shape[0], int(batch), ts, hs, _ptr(token_start), int(max_q),
+    _check(_lib.hsa_kv8_attend(ctx, q.data_ptr(), q.shape[0], batch, *_thd(q, "q"), _ptr(token_start), max_q,
                                lengths.data_ptr(), int(causal), _ptr(sel_idx), _ptr(sel_cnt),
-                               0 if sel_idx is None else sel_idx.shape[-1], out.data_ptr(), ots, ohs, _ptr(lse),
+                               0 if sel_idx is None else sel_idx.shape[-1], out.data_ptr(), *_thd(out, "out"), _ptr(lse),
                                _stream()), "hsa_kv8_attend")
 
 
@@ -739,7 +736,7 @@ class KV8Cache:
         int32 [batch + 1] where the sequences' rows differ in number, at most max_new to one.  Keys are rotated by
         `rope` at `positions` (default: their place in the sequence)."""
         most = self._rows(k, self.num_kv_heads, held, token_start, max_new, "k")
-        if v.get_device() != self._index or v.shape != k.shape:
+        if v.get_device() != self._index:
             raise ValueError("k and v must share shape and device")
         if rope is not None and (rope._index != self._index or rope.head_dim != self.head_dim):
             raise ValueError("rope: of another device or head size")
