@@ -80,15 +80,15 @@ struct Kv8AttendArgs {
 // once.  An item has as many steps as it has pages to read (times kv8 pages a step).  The steps of all items, in order,
 // are cut into equal runs, one for each CTA, from the lengths as they stand in device memory: whatever the batch holds,
 // every SM gets the same share and a captured graph serves any lengths.  (Where there are CTAs for it, each item is cut by
-// itself into parts of min_steps at least: a run that crosses items would make some wait for others.)  An item that lies in one CTA's run is written by
+// itself into parts of 2^part_log steps at least: a run that crosses items would make some wait for others.)  An item that lies in one CTA's run is written by
 // it; of one that is cut, each CTA leaves an unnormalised part in the workspace and the last to take a ticket joins them in
 // the order of the runs, which makes the result independent of which CTA that is.  Nobody waits.
 struct Kv8Work {
   int tile_rows;       // query rows of an item
   int tiles;           // tiles of a sequence with max_rows rows
-  int step_pages;
+  int step_log;        // an item takes 2^step_log pages in a step
   int half_rows;       // items of at most so many rows take twice the pages in a step
-  int min_steps;       // an item is not cut into shorter parts while there is a CTA for each part
+  int part_log;        // an item is not cut into parts of less than 2^part_log steps while there is a CTA for each part
   int item_steps;      // steps that an item costs beside its own: runs are cut as if they came before them
   int64_t items;       // batch * Hkv * tiles
   float* parts;        // [2 * CTAs][slot_floats]
@@ -121,34 +121,46 @@ struct Kv8Item {
   }
 };
 
+// Where an item lies: needs no memory.
+__device__ __forceinline__ void kv8_place(const Kv8AttendArgs& a, const Kv8Work& w, int64_t i, Kv8Item* it) {
+  const uint32_t at = static_cast<uint32_t>(i);  // (launches with 2^31 items are refused)
+  const uint32_t bh = w.tiles == 1 ? at : at / static_cast<uint32_t>(w.tiles), b = bh / static_cast<uint32_t>(a.Hkv);
+  it->tile = static_cast<int>(at - bh * static_cast<uint32_t>(w.tiles));
+  it->b = static_cast<int>(b);
+  it->h = static_cast<int>(bh - b * static_cast<uint32_t>(a.Hkv));
+  it->row0 = it->tile * w.tile_rows;
+}
+
+// What there is to do in it.
+__device__ __forceinline__ void kv8_fill(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Item* it) {
+  const int64_t bh = static_cast<int64_t>(it->b) * a.Hkv + it->h;
+  // (all that has to be read, at once)
+  const int count = a.sel_idx ? __ldg(a.sel_cnt + bh) : 0;
+  it->len = __ldg(a.lengths + it->b);
+  const bool fits = a.rows.get(it->b, &it->first, &it->n);
+  it->steps = it->pages = it->rows = 0;
+  it->list = nullptr;
+  if (!fits || it->len < 0 || it->len > static_cast<int64_t>(a.max_blocks) * kBlock) {
+    if (it->h == 0 && it->tile == 0 && blockIdx.x == 0) kv8_flag(a.status, kDevBounds);
+    return;
+  }
+  it->rows = min(w.tile_rows, it->n * a.group - it->row0);
+  if (it->rows <= 0) return;
+  if (a.sel_idx) {
+    it->list = a.sel_idx + bh * a.max_topk;
+    it->pages = min(max(count, 0), a.max_topk);
+  } else {
+    it->pages = (it->limit(a, it->rows - 1) + kBlock - 1) / kBlock;
+  }
+  const int log = w.step_log + (it->rows <= w.half_rows ? 1 : 0);
+  it->steps = max(1u, (static_cast<uint32_t>(it->pages) + (1u << log) - 1) >> log);
+}
+
 // (not inlined: a handful of places call it, seldom, and the kernels' roles share the instruction caches of an SM)
 __device__ __noinline__ static Kv8Item kv8_item(const Kv8AttendArgs& a, const Kv8Work& w, int64_t i) {
   Kv8Item it;
-  const uint32_t at = static_cast<uint32_t>(i);  // (launches with 2^31 items are refused)
-  it.tile = static_cast<int>(at % static_cast<uint32_t>(w.tiles));
-  const int bh = static_cast<int>(at / static_cast<uint32_t>(w.tiles));
-  it.b = bh / a.Hkv;
-  it.h = bh % a.Hkv;
-  it.steps = it.pages = 0;
-  it.list = nullptr;
-  const bool fits = a.rows.get(it.b, &it.first, &it.n);
-  it.len = __ldg(a.lengths + it.b);
-  it.row0 = it.tile * w.tile_rows;
-  it.rows = 0;
-  if (!fits || it.len < 0 || it.len > static_cast<int64_t>(a.max_blocks) * kBlock) {
-    if (it.h == 0 && it.tile == 0 && blockIdx.x == 0) kv8_flag(a.status, kDevBounds);
-    return it;
-  }
-  it.rows = min(w.tile_rows, it.n * a.group - it.row0);
-  if (it.rows <= 0) return it;
-  if (a.sel_idx) {
-    it.list = a.sel_idx + static_cast<int64_t>(bh) * a.max_topk;
-    it.pages = min(max(__ldg(a.sel_cnt + bh), 0), a.max_topk);
-  } else {
-    it.pages = (it.limit(a, it.rows - 1) + kBlock - 1) / kBlock;
-  }
-  const int pages = it.rows <= w.half_rows ? 2 * w.step_pages : w.step_pages;
-  it.steps = max(1, (it.pages + pages - 1) / pages);
+  kv8_place(a, w, i, &it);
+  kv8_fill(a, w, &it);
   return it;
 }
 
@@ -174,51 +186,72 @@ struct Kv8Plan {
   Kv8Segment seg[kSegments];
 };
 
+// Quotients of what is seldom past 32 bits
+__device__ __forceinline__ int64_t kv8_div(int64_t a, int64_t b) {
+  return ((a | b) >> 32) == 0 ? static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
+}
+
 __device__ __forceinline__ void kv8_cut(Kv8Segment* g, int64_t start, int64_t lo, int64_t hi, int64_t share) {
   const int64_t end = start + g->it.steps;
   g->s0 = static_cast<int>(max(lo - start, static_cast<int64_t>(0)));
   g->s1 = static_cast<int>(min(end, hi) - start);
-  g->first_cta = start >= lo && start < hi ? static_cast<int>(blockIdx.x) : static_cast<int>(start / share);
-  g->last_cta = end <= hi ? static_cast<int>(blockIdx.x) : static_cast<int>((end - 1) / share);
+  g->first_cta = start >= lo && start < hi ? static_cast<int>(blockIdx.x) : static_cast<int>(kv8_div(start, share));
+  g->last_cta = end <= hi ? static_cast<int>(blockIdx.x) : static_cast<int>(kv8_div(end - 1, share));
 }
 
-// Fills the plan; all THREADS threads call it, and meet at its end.
+// Sums over a warp's lanes up to each
+template <typename T>
+__device__ __forceinline__ T kv8_scan(T sum, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T v = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += v;
+  }
+  return sum;
+}
+
+// Waits for the kernel before and fills the plan; all THREADS threads call it, and meet at its end.  (A launch begins with cold
+// caches, and everything waits for this.  With items looked up by a call, which reads the kernel's arguments past the constant
+// cache, with their places worked out behind the wait and with two scans in turn, one query row against 777 tokens took 8.7 us
+// instead of 7.4, and one row each of 48 sequences of 300 to 8000 tokens 49.6 instead of 48.0.)
 template <int THREADS>
 __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan) {
   constexpr int W = THREADS / 32;
   __shared__ int64_t sums[W];
-  __shared__ int counts[W];
+  __shared__ int counts[W], parts_of[W];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
   const bool one = w.items <= THREADS;  // every thread has one item at most: once is enough
-  int64_t total = 0;
+  int64_t total = 0, sum = 0;
   Kv8Segment g{};
+  if (one) kv8_place(a, w, tid, &g.it);
+  if (tid == 0) {
+    plan->n = 0;
+    plan->more = false;
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (one) {
-    if (tid < w.items) g.it = kv8_item(a, w, tid);
-    // a part of an item for each CTA?
-    const int parts = (g.it.steps + w.min_steps - 1) / w.min_steps;
-    int sum = parts;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum = min(sum + v, 1 << 20);
-    }
-    if (lane == 31) counts[warp] = sum;
-    if (tid == 0) {
-      plan->n = 0;
-      plan->more = false;
+    if (tid < w.items) kv8_fill(a, w, &g.it);
+    // a part of an item for each CTA?  (counted up to more than there can be CTAs)
+    const int parts = min((static_cast<uint32_t>(g.it.steps) + (1u << w.part_log) - 1) >> w.part_log, 1024u);
+    const int upto = kv8_scan(parts, lane);
+    sum = kv8_scan(g.it.steps ? static_cast<int64_t>(g.it.steps) + w.item_steps : 0, lane);
+    if (lane == 31) {
+      parts_of[warp] = upto;
+      sums[warp] = sum;
     }
     __syncthreads();
     int before = 0, all = 0;
-#pragma unroll 4
+#pragma unroll
     for (int j = 0; j < W; ++j) {
-      if (j < warp) before += counts[j];
-      all += counts[j];
+      if (j < warp) before += parts_of[j];
+      all += parts_of[j];
     }
-    if (all <= static_cast<int>(gridDim.x)) {
-      const int first = before + sum - parts, cta = static_cast<int>(blockIdx.x);
+    if (all <= static_cast<int>(gridDim.x)) {  // (each count is right then, and steps are few)
+      const int first = before + upto - parts, cta = static_cast<int>(blockIdx.x);
       if (cta >= first && cta < first + parts) {
-        g.s0 = static_cast<int>(static_cast<int64_t>(g.it.steps) * (cta - first) / parts);
-        g.s1 = static_cast<int>(static_cast<int64_t>(g.it.steps) * (cta - first + 1) / parts);
+        g.s0 = static_cast<int>(static_cast<uint32_t>(g.it.steps * (cta - first)) / static_cast<uint32_t>(parts));
+        g.s1 = static_cast<int>(static_cast<uint32_t>(g.it.steps * (cta - first + 1)) / static_cast<uint32_t>(parts));
         g.first_cta = first;
         g.last_cta = first + parts - 1;
         plan->seg[0] = g;
@@ -227,14 +260,12 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
       __syncthreads();
       return;
     }
-    __syncthreads();
-  }
-  if (!one) {
+  } else {
     int64_t mine = 0;
 #pragma unroll 1
     for (int64_t i = tid; i < w.items; i += THREADS) {
       const int steps = kv8_item(a, w, i).steps;
-      mine += steps ? steps + w.item_steps : 0;
+      mine += steps ? static_cast<int64_t>(steps) + w.item_steps : 0;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
@@ -244,10 +275,6 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
     for (int i = 0; i < W; ++i) total += sums[i];
     __syncthreads();
   }
-  if (tid == 0) {
-    plan->n = 0;
-    plan->more = false;
-  }
   int64_t carry = 0, lo = 0, hi = 0, share = 1;
   int carried = 0;  // segments so far
 #pragma unroll 1
@@ -256,16 +283,10 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
     if (!one) {
       g.it.steps = 0;
       if (i < w.items) g.it = kv8_item(a, w, i);
+      sum = kv8_scan(g.it.steps ? static_cast<int64_t>(g.it.steps) + w.item_steps : 0, lane);
+      if (lane == 31) sums[warp] = sum;
+      __syncthreads();
     }
-    const int64_t cost = g.it.steps ? g.it.steps + w.item_steps : 0;
-    int64_t sum = cost;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += v;
-    }
-    if (lane == 31) sums[warp] = sum;
-    __syncthreads();
     int64_t before = carry, all = 0;
 #pragma unroll 4
     for (int j = 0; j < W; ++j) {
@@ -273,7 +294,7 @@ __device__ void kv8_plan(const Kv8AttendArgs& a, const Kv8Work& w, Kv8Plan* plan
       all += sums[j];
     }
     if (one) total = all;
-    share = max(static_cast<int64_t>(1), (total + gridDim.x - 1) / gridDim.x);
+    share = max(static_cast<int64_t>(1), kv8_div(total + gridDim.x - 1, gridDim.x));
     lo = min(total, share * blockIdx.x);
     hi = min(total, lo + share);
     const int64_t end = before + sum, start = end - g.it.steps;  // of its own steps

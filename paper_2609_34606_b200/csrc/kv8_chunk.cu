@@ -276,8 +276,6 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     tmem_alloc(&sm.tmem, 512);
     tmem_relinquish();
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   kv8_plan<kThreads>(a, w, &sm.plan);
   tc_fence_before();
   __syncthreads();
@@ -765,9 +763,9 @@ cudaError_t launch_kv8_chunk(const Kv8AttendArgs& a, Kv8Work w, int D, int ctas,
   w.tile_rows = 2 * kTile;
   w.tiles = static_cast<int>((rows + 2 * kTile - 1) / (2 * kTile));
   w.items = static_cast<int64_t>(a.rows.batch) * a.Hkv * w.tiles;
-  w.step_pages = 1;
+  w.step_log = 0;
   w.half_rows = kTile;
-  w.min_steps = 8;
+  w.part_log = 3;
   w.item_steps = 8;
   w.slot_floats = static_cast<int64_t>(kv8_chunk_slot(D));
   cudaLaunchConfig_t cfg{};

@@ -201,8 +201,6 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
     tmem_alloc(&sm.tmem, Sh::kCols);
     tmem_relinquish();
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   kv8_plan<Sh::kThreads>(a, w, &sm.plan);
   tc_fence_before();
   __syncthreads();
@@ -625,9 +623,9 @@ cudaError_t launch_one(const Kv8AttendArgs& a, Kv8Work w, int64_t rows, int ctas
   w.tile_rows = R;
   w.tiles = static_cast<int>((rows + R - 1) / R);
   w.items = static_cast<int64_t>(a.rows.batch) * a.Hkv * w.tiles;
-  w.step_pages = 2;
+  w.step_log = 1;
   w.half_rows = 0;
-  w.min_steps = 16;
+  w.part_log = 4;
   w.item_steps = 4;
   w.slot_floats = static_cast<int64_t>(kv8_decode_slot(D));
   cudaLaunchConfig_t cfg{};
