@@ -469,8 +469,8 @@ int hsa_kv8_create(hsa_kv8** out, const hsa_kv8_config* cfg, const hsa_kv8_buffe
  * when the new rows need it, and the codes in it follow (exactly, but for values that become subnormal); it never
  * shrinks.  Codes are rounded to nearest even from the fp32 rotated value.  With key sums: ksum[s][h][block] is
  * the sum of the block's keys, this call's before rounding and earlier ones as they are stored.
- * Appending the same rows again over the same held[] leaves the same bits.  The pages of different sequences that
- * a call writes must be distinct; full pages may be shared.
+ * Appending the same rows again over the same held[] leaves the same bits.  The pages that a call writes must be
+ * distinct, those of one sequence as those of several; pages that it does not write may be shared.
  * Values that are not finite or pass 2^60 are stored as 0 (NaN) or at 2^60 and HSA_ERR_DEVICE_NONFINITE is left in the
  * status word.  A sequence whose rows or lengths do not fit (token_start not ascending or past n_tokens, more than
  * max_new rows, held < 0, more than max_blocks blocks) is left out as a whole, a page id outside the pools as that
