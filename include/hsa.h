@@ -492,7 +492,7 @@ int hsa_kv8_append(hsa_kv8* ctx, const void* k, const void* v, int32_t n_tokens,
  * out that belong to no sequence are left as they were, and so are those of lse.  What the result is made of: queries
  * exact, but for values below 2^-10 of their row's largest, which may be off by 2^-18 of that; products exact, sums in
  * fp32; softmax weights (times their page's value scale, where a call has more than 16 query rows of a key head) rounded to
- * 8 significant bits or to 2^-21 of the largest one.  Sequences that do not fit (as above,
+ * 9 significant bits or to 2^-33 of the largest one.  Sequences that do not fit (as above,
  * lengths < 0 or past max_blocks) are left out, list entries outside [0, max_blocks) and pages outside the pools count
  * as not seen, both with HSA_ERR_DEVICE_BOUNDS; list entries behind the length see nothing. */
 int hsa_kv8_attend(hsa_kv8* ctx, const void* q, int32_t n_tokens, int32_t batch, int64_t tok_stride,

@@ -4,12 +4,16 @@
 // the tensor cores as they are -- no thread ever touches a key or a value -- and the products are turned round to have
 // keys, or dims of the values, in their long dimension:
 //     S^T [128 keys x 2R] = K [128 x d] (Qhi | Qlo)^T         K tiles as TMA leaves them, K-major
-//     O^T [d x 2R]        = V^T [d x 64 keys] (Phi | Plo)^T   V tiles as TMA leaves them, M-major, a page at a time
-// Both products need the other operand in 8 bits too.  It is given in two terms side by side, as columns of their own:
-// x = hi + lo / 16 with hi = e4m3(x), lo = e4m3(16 (x - hi)).  With the largest value of a row between 2^7 and 2^8.75 that
-// keeps 8 bits of every value, or 2^-21 of the largest (x - hi is at most 2^4; the last step of e4m3 is 2^-9).  So the bf16
-// queries stay exact unless they are below 2^-13 of their row's largest, and weights are rounded to 8 bits.  The columns are
+//     O^T [d x 3R]        = V^T [d x 64 keys] (P0 | P1 | P2)^T   V tiles as TMA leaves them, M-major, a page at a time
+// Both products need the other operand in 8 bits too.  It is given in terms side by side, as columns of their own, which are
 // added up in fp32.
+//   Queries: x = hi + lo / 16 with hi = e4m3(x), lo = e4m3(16 (x - hi)).  With the largest value of a row between 2^7 and 2^8
+// that keeps 8 bits of every value, or 2^-21 of the largest (x - hi is at most 2^4; the last step of e4m3 is 2^-9).  So the bf16
+// queries stay exact unless they are below 2^-13 of their row's largest.
+//   Weights: w = t0 + t1 / 8 + t2 / 64, each the e5m2 nearest to what those before it leave (at most an eighth of it): 9 bits of
+// every weight down to 2^-14, 2^-23 below that.  The largest is 2^12 when the reference is set and stays below 2^15.8, so that 9
+// bits are left 2^-26 below it, and 2^-35 of it is the least that counts.  (Two e4m3 terms, whose weights ended at 2^-21
+// of the largest: behind a key 15 nats above 1500 others the result lost a quarter, and an error of 2^-21 a key adds up.)
 //
 // One thread holds one key: y = S * scales, weight 2^(y - ref).  ref[row] is what the largest y was when it was set; as long as
 // no y passes it by kSlack nothing but a vote is needed, else the maxima are taken anew.  The same thread then holds one
@@ -34,13 +38,14 @@ namespace hsa {
 
 namespace {
 
-constexpr float kShift = 7.f;   // the largest weight is 2^7 when the reference is set ...
-constexpr float kSlack = 1.75f; // ... and may grow to 2^8.75 < 448 before it is set anew
+constexpr float kShift = 12.f;  // the largest weight is 2^12 when the reference is set ...
+constexpr float kSlack = 3.75f; // ... and may grow to 2^15.75 < 57344, the largest e5m2, before it is set anew
 
 // R: rows of an item.  A step is a tile of 128 keys, two pages.
 template <int D, int R>
 struct DecodeShape {
-  static constexpr int N = R < 8 ? 16 : 2 * R;           // columns of the products: first terms, then second ones (16 at least)
+  static constexpr int N = R < 8 ? 16 : 2 * R;           // columns of the first products: first terms, then second ones (16 at least)
+  static constexpr int NP = R < 8 ? 16 : R == 8 ? 32 : 3 * R;  // of the second ones: three terms (a multiple of 16)
   static constexpr int kGroups = 2;
   static constexpr int kThreads = 128 + 128 * kGroups;
   static constexpr int kPage = kBlock * D;               // bytes of a page tile
@@ -48,7 +53,8 @@ struct DecodeShape {
   static constexpr int kStages = D == 64 ? 12 : 6;
   static constexpr uint32_t kS = 0;                      // TMEM columns: S of two steps, then O of their pages
   static constexpr uint32_t kO = 2 * N;
-  static constexpr uint32_t kCols = 6 * N <= 128 ? 128 : 6 * N <= 256 ? 256 : 512;
+  static constexpr uint32_t kCols = 2 * N + 4 * NP <= 128 ? 128 : 256;
+  static_assert(2 * N + 4 * NP <= 256);
 };
 
 template <int D, int R>
@@ -56,7 +62,7 @@ struct DecodeSmem {
   using Sh = DecodeShape<D, R>;
   uint8_t k[Sh::kStages][Sh::kStage];
   uint8_t v[Sh::kStages][Sh::kStage];
-  uint8_t p[2][Sh::N * 128];               // weights: [hi rows | lo rows][128 keys]
+  uint8_t p[2][Sh::NP * 128];              // weights: [rows of a term, three times][128 keys]
   uint8_t q[2][Sh::N * D];
   float other[R * (D + 2)];  // sums of the group that does not write the item: [R][D], references, sums of weights
   float qscale[2][R];
@@ -104,6 +110,31 @@ __device__ __forceinline__ void two_terms(float a, float b, uint32_t* hi, uint32
   *lo = __nv_cvt_float2_to_fp8x2(make_float2((a - f.x) * 16.f, (b - f.y) * 16.f), __NV_SATFINITE, __NV_E4M3);
 }
 
+// Two weights (below 65504) as three e5m2 terms each: bytes 0, 1 of each result.  The 11 bits of fp16 are more than the terms hold,
+// and so is its last step of 2^-24; what is left behind a term, and eight times that, is exact in it.
+__device__ __forceinline__ void three_terms(float a, float b, uint32_t* t0, uint32_t* t1, uint32_t* t2) {
+  asm("{\n"
+      ".reg .b32 x, z, e;\n"
+      ".reg .b16 t;\n"
+      "mov.b32 e, 0x48004800;\n"
+      "cvt.rn.f16x2.f32 x, %4, %3;\n"
+      "cvt.rn.satfinite.e5m2x2.f16x2 t, x;\n"
+      "cvt.u32.u16 %0, t;\n"
+      "cvt.rn.f16x2.e5m2x2 z, t;\n"
+      "sub.rn.f16x2 x, x, z;\n"
+      "mul.rn.f16x2 x, x, e;\n"
+      "cvt.rn.satfinite.e5m2x2.f16x2 t, x;\n"
+      "cvt.u32.u16 %1, t;\n"
+      "cvt.rn.f16x2.e5m2x2 z, t;\n"
+      "sub.rn.f16x2 x, x, z;\n"
+      "mul.rn.f16x2 x, x, e;\n"
+      "cvt.rn.satfinite.e5m2x2.f16x2 t, x;\n"
+      "cvt.u32.u16 %2, t;\n"
+      "}\n"
+      : "=r"(*t0), "=r"(*t1), "=r"(*t2)
+      : "f"(a), "f"(b));
+}
+
 template <int COLS>
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r) {
   if constexpr (COLS == 16) tmem_ld16(addr, *reinterpret_cast<uint32_t(*)[16]>(r));
@@ -111,6 +142,35 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r) {
   else {
     tmem_ld32(addr, *reinterpret_cast<uint32_t(*)[32]>(r));
     tmem_ld32(addr + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
+  }
+}
+
+// The three terms of R rows, added up.
+template <int R>
+__device__ __forceinline__ void tmem_load_terms(uint32_t addr, float (&sum)[R]) {
+  if constexpr (R <= 4) {
+    uint32_t x[16];
+    tmem_ld16(addr, x);
+    tc_wait_ld();
+#pragma unroll
+    for (int r = 0; r < R; ++r) sum[r] = fmaf(fmaf(__uint_as_float(x[2 * R + r]), 0.125f, __uint_as_float(x[R + r])), 0.125f, __uint_as_float(x[r]));
+  } else if constexpr (R == 8) {
+    uint32_t x[16], y[8];
+    tmem_ld16(addr, x);
+    tmem_ld8(addr + 16, y);
+    tc_wait_ld();
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sum[r] = fmaf(fmaf(__uint_as_float(y[r]), 0.125f, __uint_as_float(x[8 + r])), 0.125f, __uint_as_float(x[r]));
+  } else {  // (one after the other: the registers are few)
+    static_assert(R == 16);
+#pragma unroll
+    for (int t = 2; t >= 0; --t) {
+      uint32_t x[16];
+      tmem_ld16(addr + t * 16, x);
+      tc_wait_ld();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[r] = t == 2 ? __uint_as_float(x[r]) : fmaf(sum[r], 0.125f, __uint_as_float(x[r]));
+    }
   }
 }
 
@@ -172,7 +232,7 @@ __global__ void __launch_bounds__((DecodeShape<D, R>::kThreads), 1)
 kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant__ Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using Sh = DecodeShape<D, R>;
   using Smem = DecodeSmem<D, R>;
-  constexpr int N = Sh::N, kStages = Sh::kStages, kGroups = Sh::kGroups;
+  constexpr int N = Sh::N, NP = Sh::NP, kStages = Sh::kStages, kGroups = Sh::kGroups;
   extern __shared__ uint8_t smem_raw[];
   Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
@@ -304,7 +364,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
     if (mbar_poll(&sm.done[0], 0, 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
   } else if (warp == 3) {
     // ---- second products, a page at a time (of pages that are not there too: nobody looks at what they give)
-    constexpr uint32_t id = idesc_e4m3(128, N, 1, 0);
+    constexpr uint32_t id = idesc_e4m3(128, NP, 1, 0) | 1u << 10;  // (B: e5m2)
     // (head_dim 64: the upper half of M reads what lies a page further, whatever that is; those lanes of the accumulator
     // are not looked at)
     const uint32_t v0 = row_desc_lo(smem_u32(sm.v)) | (D == 128 ? 0u : static_cast<uint32_t>(Sh::kPage >> 4) << 16),
@@ -314,7 +374,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
       const uint32_t steps = warp_uniform(walk.g.s1 - walk.g.s0);
 #pragma unroll 1
       for (uint32_t s = 0; s < steps; ++s, ++n) {
-        const uint32_t b = n & 1, v = v0 + st * (Sh::kStage / 16), p = p0 + b * (N * 128 / 16);
+        const uint32_t b = n & 1, v = v0 + st * (Sh::kStage / 16), p = p0 + b * (NP * 128 / 16);
         wait(&sm.v_full[st], round & 1);
         wait(&sm.p_full[b], (n / 2) & 1);
         tc_fence_after();
@@ -323,7 +383,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
           for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
             for (int half = 0; half < 2; ++half)  // 32 keys: rows of V, bytes of a row of P
-              mma_f8_lo(tm + Sh::kO + (b * 2 + pg) * N, v + (pg * Sh::kPage + half * 32 * D) / 16, p + (pg * 64 + half * 32) / 16,
+              mma_f8_lo(tm + Sh::kO + (b * 2 + pg) * NP, v + (pg * Sh::kPage + half * 32 * D) / 16, p + (pg * 64 + half * 32) / 16,
                         row_desc_hi<D>(), row_desc_hi<128>(), id, half);
           tc_commit(&sm.empty[st]);
           tc_commit(&sm.p_free[b]);
@@ -428,11 +488,10 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         for (int pg = 0; pg < 2; ++pg) {
           const float vs = pg ? vs1 : vs0;
           if (vs > 0.f) {
-            uint32_t x[N];
-            tmem_load<N>(tmem + lanes + Sh::kO + ((i & 1) * 2 + pg) * N, x);
-            tc_wait_ld();
+            float x[R];
+            tmem_load_terms<R>(tmem + lanes + Sh::kO + ((i & 1) * 2 + pg) * NP, x);
 #pragma unroll
-            for (int r = 0; r < R; ++r) o[r] = fmaf(fmaf(__uint_as_float(x[N / 2 + r]), kLow, __uint_as_float(x[r])), vs, o[r]);
+            for (int r = 0; r < R; ++r) o[r] = fmaf(x[r], vs, o[r]);
           }
         }
         tc_fence_before();
@@ -497,12 +556,13 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
           const float p0 = ex2(y[r] + (kShift - ref[r])), p1 = ex2(y[r + 1] + (kShift - ref[r + 1]));
           l[r] += p0;
           l[r + 1] += p1;
-          uint32_t hi, lo;
-          two_terms(p0, p1, &hi, &lo);
-          p[swizzled<128>(r, key)] = static_cast<uint8_t>(hi);
-          p[swizzled<128>(r + 1, key)] = static_cast<uint8_t>(hi >> 8);
-          p[swizzled<128>(N / 2 + r, key)] = static_cast<uint8_t>(lo);
-          p[swizzled<128>(N / 2 + r + 1, key)] = static_cast<uint8_t>(lo >> 8);
+          uint32_t t[3];
+          three_terms(p0, p1, &t[0], &t[1], &t[2]);
+#pragma unroll
+          for (int i = 0; i < 3; ++i) {
+            p[swizzled<128>(i * R + r, key)] = static_cast<uint8_t>(t[i]);
+            p[swizzled<128>(i * R + r + 1, key)] = static_cast<uint8_t>(t[i] >> 8);
+          }
         }
         fence_proxy_async_smem();
         mbar_arrive(&sm.p_full[b]);
