@@ -488,7 +488,8 @@ int hsa_kv8_append(hsa_kv8* ctx, const void* k, const void* v, int32_t n_tokens,
  *   sel_idx_dev      device int32[batch][num_kv_heads][max_topk] block lists, or NULL: every block
  *   sel_cnt_dev      device int32[batch][num_kv_heads] their lengths (clamped to 0..max_topk)
  *   lse_dev          device fp32 [n_tokens][num_heads] receiving ln sum_j exp(scale q . k_j), or NULL
- * A block that a list names twice counts twice.  A query that sees nothing gets zeros and an lse of -inf.  Rows of
+ * A block that a list names twice counts twice.  A query that sees nothing gets zeros and an lse of -inf; one whose scores (in
+ * powers of two) pass the range of fp32 has no defined result, and spoils no other.  Rows of
  * out that belong to no sequence are left as they were, and so are those of lse.  What the result is made of: queries
  * exact, but for values below 2^-10 of their row's largest, which may be off by 2^-18 of that; products exact, sums in
  * fp32; softmax weights (times their page's value scale, where a call has more than 16 query rows of a key head) rounded to

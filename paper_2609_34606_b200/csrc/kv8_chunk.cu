@@ -12,6 +12,11 @@
 // value scale in what is added in the exponent (and taken out of the sum of weights again).  So P holds weight times value scale.
 // It is set up to have its largest value at 2^8 and may grow to 2^15; what fp16 cannot hold beside that, below 2^-25, is less than
 // 2^-33 of the largest contribution.
+// A row's reference has two parts, of the scores (`top`) and of the scales (`base`): a weight is 2^((s c - top) + (lv - base)).  Up to
+// 2^22 both are whole numbers, so that (lv - base) - top is exact and one fma makes the exponent.  Above that fp32 leaves scores no
+// fraction, and the exact product in an fma would differ from a rounded reference by up to half a step of it, which passes what fp16
+// holds from 2^27 on: there the product is rounded first, the largest score gives a difference of 0, and only then the scales'
+// part is added.
 //
 // An item has 256 rows, two tiles of 128, so that every page that is read and turned into fp16 serves both.  A tile's S has
 // two buffers of a page's 64 keys: the products of a page run while the softmax is at the page before it.  (With one buffer of
@@ -42,6 +47,7 @@ constexpr int kThreads = 512;
 constexpr int kTile = 128;          // rows of a tile
 constexpr float kMost = 32768.f;    // what a page's 64 keys may add up to in P before a row's reference is set anew
 constexpr float kShift = 8.f;       // ... to have the largest at 2^8
+constexpr float kFar = 4194304.f;   // 2^22: references up to here take part in the product's own rounding
 constexpr int kMetas = 16;
 
 template <int D>
@@ -56,7 +62,7 @@ struct ChunkSmem {
   uint8_t vc[kVStages][kPage];         // codes
   uint8_t vb[kBStages][kPage * 2];     // fp16, [64 dims][key][64 dims]
   float qscale[2 * kTile];
-  float other_ref[2][kTile], other_sum[2][kTile];
+  float other_top[2][kTile], other_base[2][kTile], other_sum[2][kTile];
   PageMeta meta[kMetas];
   int last[2];
   uint64_t k_full[kKStages], k_empty[kKStages], vc_full[kVStages], vc_empty[kVStages], vb_full[kBStages], vb_empty[kBStages];
@@ -103,6 +109,23 @@ __device__ __forceinline__ float weights(uint32_t* s, float c, float nref, uint3
   }
   const float2 a = unpair(sum[0]), b = unpair(sum[1]);
   return (a.x + a.y) + (b.x + b.y);
+}
+
+// The same where a row of the warp is far: 2^(((s * c + n1) + n2) + n3).  (Summed in the same order: rows that are not far get what
+// they get from weights().)
+__device__ __forceinline__ float weights_far(uint32_t* s, float c, float n1, float n2, float n3, uint32_t* w) {
+  float sum[2][2] = {};
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    float e[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      e[j] = ex2((fmaf(__uint_as_float(s[2 * i + j]), c, n1) + n2) + n3);
+      sum[i & 1][j] += e[j];
+    }
+    asm("cvt.rn.f16x2.f32 %0, %2, %1;" : "=r"(w[i]) : "f"(e[0]), "f"(e[1]));
+  }
+  return (sum[0][0] + sum[0][1]) + (sum[1][0] + sum[1][1]);
 }
 
 // two e4m3 codes as fp16
@@ -197,18 +220,32 @@ __device__ __forceinline__ float two_terms(const __nv_bfloat16* q_in, int64_t fr
 __device__ __forceinline__ void tiles_sync() { asm volatile("barrier.cta.sync 3, 256;" ::: "memory"); }
 __device__ __forceinline__ void tile_sync(int tile) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(1 + tile) : "memory"); }
 
-// A part: a tile's O (fp32, unnormalised) as [D / 4][row][4], the rows' references and sums.
+// A row's reference.
+struct RowRef {
+  float top = kNone, base = 0.f;
+  __device__ __forceinline__ static RowRef load(const float* p) { return RowRef{__ldcg(p), __ldcg(p + kTile)}; }
+  __device__ __forceinline__ bool far() const { return fabsf(top) > kFar && top != kNone; }
+  __device__ __forceinline__ float above(const RowRef& o) const { return (top - o.top) + (base - o.base); }  // exponent of what counted by this one
+  __device__ __forceinline__ void raise(const RowRef& o) {  // (in the order of the CTAs: the result is the same whoever joins)
+    if (o.above(*this) > 0.f) *this = o;
+  }
+  // ln of a sum of weights counted by it
+  __device__ __forceinline__ float lse(float l) const { return l == 0.f ? -INFINITY : (top + (base + log2f(l))) * 0.69314718055994531f; }
+};
+
+// A part: a tile's O (fp32, unnormalised) as [D / 4][row][4], both parts of the rows' references, and sums.
 template <int D>
 __device__ __forceinline__ float* part_of(const Kv8Work& w, int64_t slot, int tile) {
-  return w.parts + slot * w.slot_floats + tile * (kTile * (D + 2));
+  return w.parts + slot * w.slot_floats + tile * (kTile * (D + 3));
 }
 
 // Dims d0 .. d1 of a row of an item that is shared by CTAs, from all their parts.
 template <int D>
 __device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w, const Kv8Segment& g, int t, int r, int d0, int d1, __nv_bfloat16* out,
                                         int64_t lse_at) {
-  float m = kNone, l = 0.f;
-  for (int j = g.first_cta; j <= g.last_cta; ++j) m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
+  RowRef ref;
+  float l = 0.f;
+  for (int j = g.first_cta; j <= g.last_cta; ++j) ref.raise(RowRef::load(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
 #pragma unroll 1
   for (int c = d0; c < d1; c += 32) {
     float4 o[8];
@@ -218,8 +255,8 @@ __device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w
 #pragma unroll 1
     for (int j = g.first_cta; j <= g.last_cta; ++j) {
       const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t);
-      const float f = ex2(__ldcg(p + kTile * D + r) - m);
-      l = fmaf(__ldcg(p + kTile * D + kTile + r), f, l);
+      const float f = ex2(RowRef::load(p + kTile * D + r).above(ref));
+      l = fmaf(__ldcg(p + kTile * D + 2 * kTile + r), f, l);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + (c / 4 + k) * kTile + r);
@@ -236,7 +273,7 @@ __device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w
           make_uint4(pack_bf16(o[k].x * inv, o[k].y * inv), pack_bf16(o[k].z * inv, o[k].w * inv),
                      pack_bf16(o[k + 1].x * inv, o[k + 1].y * inv), pack_bf16(o[k + 1].z * inv, o[k + 1].w * inv));
   }
-  if (a.lse && d0 == 0) a.lse[lse_at] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+  if (a.lse && d0 == 0) a.lse[lse_at] = ref.lse(l);
 }
 
 template <int D>
@@ -511,7 +548,9 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         __syncwarp();
       }
       const float qs = sm.qscale[row];
-      float ref = kNone, l = 0.f;
+      RowRef ref;
+      float l = 0.f;
+      bool far = false;
 #pragma unroll 1
       for (int u = 0; u < units; ++u, ++n) {
         const uint32_t b = (n & 1) * 2 + t, col_s = tmem + lanes + kColS + b * 64;
@@ -536,36 +575,43 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         };
         tc_wait_ld();
         if (__builtin_expect(masked, 0)) mask();
-        float more = weights(x, c, lv - ref, p);
+        float more = weights(x, c, (lv - ref.base) - ref.top, p);
         // The sum tells whether the reference is still good (at an item's begin it is not: the sum is infinite).  The maximum of the
-        // scores is looked for only where it is not.
-        if (__builtin_expect(__any_sync(0xffffffffu, more > kMost), 0)) {
+        // scores is looked for only where it is not, and for rows that are far.
+        if (__builtin_expect(__any_sync(0xffffffffu, more > kMost || far), 0)) {
           load();
           tc_wait_ld();
           if (masked) mask();
           float top = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 64; i += 2) top = max3(top, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-          top = top * c + (lv - kShift);
-          const float to = more > kMost && top > ref ? top : ref, f = ex2(ref - to);
-          ref = to;
-          l *= f;
-          if (u > 0) {
-            wait(&sm.pv_done[((n - 1) & 1) * 2 + t], ((n - 1) / 2) & 1);  // (those before have been, or these scores were not there)
-            __syncwarp();
-            tc_fence_after();
+          top *= c;
+          const bool up = far ? (top - ref.top) + (lv - ref.base) > kShift : more > kMost;
+          const RowRef to{up ? rintf(top) : ref.top, up ? lv - kShift : ref.base};
+          if (__any_sync(0xffffffffu, up)) {
+            const float f = up ? ex2(ref.above(to)) : 1.f;
+            l *= f;
+            if (u > 0) {
+              wait(&sm.pv_done[((n - 1) & 1) * 2 + t], ((n - 1) / 2) & 1);  // (those before have been, or these scores were not there)
+              __syncwarp();
+              tc_fence_after();
 #pragma unroll 1
-            for (int i = 0; i < D; i += 16) {
-              uint32_t o[16];
-              tmem_ld16(col_o + i, o);
-              tc_wait_ld();
+              for (int i = 0; i < D; i += 16) {
+                uint32_t o[16];
+                tmem_ld16(col_o + i, o);
+                tc_wait_ld();
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st16(col_o + i, o);
+                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                tmem_st16(col_o + i, o);
+              }
             }
           }
+          ref = to;
+          far = ref.far();
           // (rows whose reference stays get the weights they had)
-          more = weights(x, c, lv - ref, p);
+          const float scales = lv - ref.base;
+          if (__any_sync(0xffffffffu, far)) more = weights_far(x, c, far ? -0.f : scales - ref.top, far ? -ref.top : 0.f, far ? scales : 0.f, p);
+          else more = weights(x, c, scales - ref.top, p);
         }
         tmem_st32(col_s, p);
         l = fmaf(more, __uint_as_float((254u << 23) - (__float_as_uint(meta.vs) & 0x7f800000u)), l);  // 1 / vs
@@ -593,14 +639,16 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
 #pragma unroll
           for (int j = 0; j < 32; ++j) sm.other[i + j][r] = __uint_as_float(o[j]);
         }
-        sm.other_ref[t][r] = ref;
+        sm.other_top[t][r] = ref.top;
+        sm.other_base[t][r] = ref.base;
         sm.other_sum[t][r] = l;
         tiles_sync();
-        const float r0 = sm.other_ref[0][r], r1 = sm.other_ref[1][r], to = fmaxf(r0, r1), f0 = ex2(r0 - to), f1 = ex2(r1 - to);
+        const RowRef r0{sm.other_top[0][r], sm.other_base[0][r]}, r1{sm.other_top[1][r], sm.other_base[1][r]};
+        const float above = r1.above(r0), f0 = above > 0.f ? ex2(-above) : 1.f, f1 = above > 0.f ? 1.f : ex2(above);
         down = t == 0 ? f0 : f1;
         take = t == 0 ? f1 : f0;
         l = fmaf(sm.other_sum[1][r], f1, sm.other_sum[0][r] * f0);
-        ref = to;
+        ref = above > 0.f ? r1 : r0;
       }
       // Is the item shared with other CTAs, then the last one of them joins the parts, in the order of the CTAs whoever that is, its
       // own from where it is.  The others leave theirs in the workspace.
@@ -622,17 +670,17 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       const bool writes = !others || joins;  // the item's rows, else a part
       float own = 1.f;                       // what this CTA's O counts
       if (joins) {
-        float m = ref;
+        RowRef m;
 #pragma unroll 4
         for (int j = g.first_cta; j <= g.last_cta; ++j)
-          if (j != static_cast<int>(blockIdx.x)) m = fmaxf(m, __ldcg(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
-        own = ex2(ref - m);
+          m.raise(j == static_cast<int>(blockIdx.x) ? ref : RowRef::load(part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r));
+        own = ex2(ref.above(m));
         float sum = 0.f;
 #pragma unroll 1
         for (int j = g.first_cta; j <= g.last_cta; ++j) {
           const float* p = part_of<D>(w, Kv8Segment::slot_of(j, g.first_cta), t) + kTile * D + r;
           const bool here = j == static_cast<int>(blockIdx.x);
-          sum = fmaf(here ? l : __ldcg(p + kTile), here ? own : ex2(__ldcg(p) - m), sum);
+          sum = fmaf(here ? l : __ldcg(p + 2 * kTile), here ? own : ex2(RowRef::load(p).above(m)), sum);
         }
         l = sum;
         ref = m;
@@ -667,7 +715,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
             float4 v[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(p) + (i / 4 + k) * kTile + r);
-            const float f = ex2(__ldcg(p + kTile * D + r) - ref);
+            const float f = ex2(RowRef::load(p + kTile * D + r).above(ref));
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               sum[4 * k] = fmaf(v[k].x, f, sum[4 * k]);
@@ -711,10 +759,11 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       }
       if (real) {
         if (writes) {
-          if (a.lse && d0 == 0) a.lse[tok * a.Hq + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.69314718055994531f;
+          if (a.lse && d0 == 0) a.lse[tok * a.Hq + head] = ref.lse(l);
         } else {
-          __stcg(part + kTile * D + r, ref);
-          __stcg(part + kTile * D + kTile + r, l);
+          __stcg(part + kTile * D + r, ref.top);
+          __stcg(part + kTile * D + kTile + r, ref.base);
+          __stcg(part + kTile * D + 2 * kTile + r, l);
         }
       }
       if (same) tiles_sync();
@@ -750,7 +799,7 @@ constexpr size_t smem_bytes() {
 
 }  // namespace
 
-size_t kv8_chunk_slot(int D) { return static_cast<size_t>(2 * kTile) * (D + 2); }
+size_t kv8_chunk_slot(int D) { return static_cast<size_t>(2 * kTile) * (D + 3); }
 
 cudaError_t kv8_chunk_init(int D) {
   return D == 128 ? cudaFuncSetAttribute(kv8_chunk_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<128>()))

@@ -223,7 +223,7 @@ __device__ __forceinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work
     const float down = tot == 0.f ? 0.f : 1.f / tot;
     *reinterpret_cast<uint2*>(a.out + tok * a.ots + head * a.ohs + f * 4) =
         make_uint2(pack_bf16(sum.x * down, sum.y * down), pack_bf16(sum.z * down, sum.w * down));
-    if (a.lse && f == 0) a.lse[tok * a.Hq + head] = tot == 0.f ? -INFINITY : (m - kShift + log2f(tot)) * 0.69314718055994531f;
+    if (a.lse && f == 0) a.lse[tok * a.Hq + head] = tot == 0.f ? -INFINITY : (m + (log2f(tot) - kShift)) * 0.69314718055994531f;
   }
 }
 
@@ -523,7 +523,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
               if (pos >= sm.limit[qb][r]) y[r] = -INFINITY;
           }
 #pragma unroll
-          for (int r = 0; r < R; ++r) over |= y[r] > ref[r] + kSlack;
+          for (int r = 0; r < R; ++r) over |= y[r] - ref[r] > kSlack;  // (ref + kSlack would be rounded where scores pass 2^22)
         }
         const float vs0_now = sm.meta[st][0].vs, vs1_now = sm.meta[st][1].vs;
         tc_fence_before();
@@ -541,7 +541,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
           for (int r = 0; r < R; ++r) {
             const float* red = &sm.red[group][0][r];
             const float top = fmaxf(fmaxf(red[0], red[R]), fmaxf(red[2 * R], red[3 * R]));
-            const float to = top > ref[r] + kSlack ? top : ref[r], c = ex2(ref[r] - to);
+            const float to = top - ref[r] > kSlack ? top : ref[r], c = ex2(ref[r] - to);
             ref[r] = to;
             l[r] *= c;
             o[r] *= c;
@@ -553,7 +553,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         uint8_t* p = sm.p[b];
 #pragma unroll
         for (int r = 0; r < R; r += 2) {
-          const float p0 = ex2(y[r] + (kShift - ref[r])), p1 = ex2(y[r + 1] + (kShift - ref[r + 1]));
+          const float p0 = ex2((y[r] - ref[r]) + kShift), p1 = ex2((y[r + 1] - ref[r + 1]) + kShift);
           l[r] += p0;
           l[r + 1] += p1;
           uint32_t t[3];
@@ -623,7 +623,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
               const int h = it.h * a.group + head;
               if (key < D) a.out[tok * a.ots + h * a.ohs + key] = __float2bfloat16_rn(l[r] == 0.f ? 0.f : o[r] / l[r]);
               if (a.lse && key == 0)
-                a.lse[static_cast<int64_t>(tok) * a.Hq + h] = l[r] == 0.f ? -INFINITY : (ref[r] - kShift + log2f(l[r])) * 0.69314718055994531f;
+                a.lse[static_cast<int64_t>(tok) * a.Hq + h] = l[r] == 0.f ? -INFINITY : (ref[r] + (log2f(l[r]) - kShift)) * 0.69314718055994531f;
             } else {
               if (key < D) part[r * D + key] = o[r];
               if (key == 0) {

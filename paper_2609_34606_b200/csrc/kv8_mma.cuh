@@ -8,7 +8,7 @@
 
 namespace hsa {
 
-constexpr float kNone = -1e30f; // reference of a row that has seen nothing
+constexpr float kNone = -3.402823466e38f; // reference of a row that has seen nothing: no score of fp32 is below it
 
 struct PageMeta {
   int pos;      // position of the page's first token; < 0: nothing to see

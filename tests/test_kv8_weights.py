@@ -50,3 +50,77 @@ def test_a_dominant_key_leaves_the_others_their_weight(cuda_device, d, Hq, Hkv, 
     score = 2.0 ** -16 * float(q.abs().max()) * float(k.double().abs().sum(-1).max()) * 1.07 / math.sqrt(d) + 2.0 ** -20
     check(got, lse, reference(c, q, True), score)
     assert c.cache.device_status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", ROWS)
+@pytest.mark.parametrize("power", [12, 22, 28, 38, 50, math.inf])
+def test_one_huge_key(cuda_device, d, Hq, Hkv, n, power):
+    """A key whose scores pass 2^power: rows that it points at get its value alone, rows that it points away from the others'
+    result.  (inf: as it is stored, 2^60.)"""
+    c = Case(cuda_device, Hq, Hkv, d, [700], seed=21)
+    k, v = c.randn(700, Hkv, d), c.randn(700, Hkv, d)
+    for b in range(0, 700, 64):
+        v[b:b + 64] *= 2.0 ** (b // 64 % 5 * 3 - 6)
+    k[70] *= 2.0 ** min(power, 50)
+    k[70, :, 0] = 2.0 ** power * 40
+    q = c.randn(n, Hq, d)
+    q[..., 0] = torch.where(torch.rand(n, Hq, generator=c.g) < 0.5, -4.0, 4.0)
+    c.append([700], k=k, v=v, twin=False)
+    assert c.cache.device_status() == (0 if power < 60 else -7)
+    c.take_gpu_state()
+    _, got, lse = c.attend([n], True, q=q, check=False)
+    ref = reference(c, q, True)
+    k[70] = 0
+    score = 2.0 ** -16 * float(q.abs().max()) * float(k.double().abs().sum(-1).max()) * 1.07 / math.sqrt(d) + 2.0 ** -20
+    # rows that the huge key points at: nothing else counts; its score is off by 2^-14 of itself (short products, sums of 128 terms)
+    hit = np.abs(ref[1]) > 1000
+    assert hit.any() and not hit.all() or n * Hq < 4
+    part = lambda rows: (got.cpu()[rows], lse.cpu()[rows], [x[rows] for x in ref])
+    check(*part(~hit), score)
+    o, l, mine = part(hit)
+    check(o, torch.from_numpy(mine[1]), mine, 0.0)
+    assert (np.abs(l.double().numpy() - mine[1]) <= 2.0 ** -14 * np.abs(mine[1])).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", ROWS)
+@pytest.mark.parametrize("power,q_power", [(0, 0), (21, 0), (30, 0), (45, 0), (59, 0), (59, 45)])
+@pytest.mark.parametrize("tokens", [650, 9000])
+def test_ties_of_any_size(cuda_device, d, Hq, Hkv, n, power, q_power, tokens):
+    """All keys alike: every row is the mean of the values it sees, whatever the scores are, over pages of different value scales."""
+    c = Case(cuda_device, Hq, Hkv, d, [tokens], seed=22, max_tokens=tokens)
+    k, v = c.randn(1, Hkv, d) * 2.0 ** power, 1 + c.randn(tokens, Hkv, d, scale=0.5)
+    k = k.clamp(-2.0 ** 59, 2.0 ** 59).expand(tokens, Hkv, d).contiguous()
+    for b in range(0, tokens, 64):
+        v[b:b + 64] *= 2.0 ** (b // 64 % 5 * 3 - 6)
+    q = c.randn(n, Hq, d) * 2.0 ** q_power
+    c.append([tokens], k=k, v=v, twin=False)
+    c.take_gpu_state()
+    _, got, lse = c.attend([n], True, q=q, check=False)
+    ref = reference(c, q, True)
+    check(got, torch.from_numpy(ref[1]), ref, 0.0)
+    size = float(q.double().abs().max()) * float(k.double().abs().sum(-1).max()) * 1.07 / math.sqrt(d)
+    assert (np.abs(lse.double().cpu().numpy() - ref[1]) <= 2.0 ** -16 * size + 2.0 ** -20 * (1 + np.abs(ref[1]))).all()
+    assert c.cache.device_status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", ROWS)
+@pytest.mark.parametrize("high", [0, 1])
+@pytest.mark.parametrize("power", [21, 24, 25, 26])
+def test_scores_one_step_of_fp32_apart(cuda_device, d, Hq, Hkv, n, high, power):
+    """Scores of 1.5 * 2^power, in powers of two, where fp32 steps by 2^(power - 23): a few keys are one step above the others."""
+    c = Case(cuda_device, Hq, Hkv, d, [900], seed=23, softmax_scale=math.log(2))
+    k, v = torch.zeros(900, Hkv, d, dtype=torch.bfloat16), 1 + c.randn(900, Hkv, d, scale=0.5)
+    k[:, :, 0] = 1.5 * 2.0 ** (power - 10)
+    few = torch.arange(900) % 128 == 77 if high else torch.arange(900) // 64 == 6
+    k[few, :, 1] = 2.0 ** (power - 23)
+    q = torch.zeros(n, Hq, d, dtype=torch.bfloat16)
+    q[:, :, 0], q[:, :, 1] = 2 ** 10, 1
+    c.append([900], k=k, v=v, twin=False)
+    c.take_gpu_state()
+    _, got, lse = c.attend([n], False, q=q, check=False)
+    ref = reference(c, q, False)
+    check(got, torch.from_numpy(ref[1]), ref, 0.0)
+    assert (np.abs(lse.double().cpu().numpy() - ref[1]) <= 2.0 ** -22 * np.abs(ref[1])).all()
