@@ -885,6 +885,7 @@ int hsa_device_status(hsa_ctx* ctx, int32_t* status_out) {
   // ticket, which leaves its list's counter short: they start over too.
   if (e == cudaSuccess && v != 0) e = cudaMemset(ws + ctx->lay.status + 8, 0, 8);
   if (e == cudaSuccess && v != 0 && ctx->lay.fwd_splits > 1) e = cudaMemset(ws + ctx->lay.part_ticket, 0, ticket_bytes(&ctx->cfg));
+  if (e == cudaSuccess && v != 0) e = cudaDeviceSynchronize();  // (the fills are not ordered with what other streams are given next)
   if (e != cudaSuccess) return cuda_fail(ctx, e);
   *status_out = v;
   return HSA_OK;
@@ -898,6 +899,7 @@ int hsa_safe_pass_tiles(hsa_ctx* ctx, int64_t* count_out) {
   int32_t v = 0;
   e = cudaMemcpy(&v, ws + ctx->lay.status + 4, 4, cudaMemcpyDeviceToHost);
   if (e == cudaSuccess && v != 0) e = cudaMemset(ws + ctx->lay.status + 4, 0, 4);
+  if (e == cudaSuccess && v != 0) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return cuda_fail(ctx, e);
   *count_out = v;
   return HSA_OK;

@@ -227,6 +227,7 @@ int hsa_kv8_device_status(hsa_kv8* ctx, int32_t* status_out) {
   cudaError_t e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = cudaMemcpy(&v, ctx->buf.workspace, 4, cudaMemcpyDeviceToHost);
   if (e == cudaSuccess && v != 0) e = cudaMemset(ctx->buf.workspace, 0, kStatusBytes + kTicketBytes);
+  if (e == cudaSuccess && v != 0) e = cudaDeviceSynchronize();  // (the fill is not ordered with what other streams are given next)
   if (e != cudaSuccess) return cuda_fail(ctx, e);
   *status_out = v;
   return HSA_OK;

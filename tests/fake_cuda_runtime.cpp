@@ -25,6 +25,7 @@ std::map<std::pair<int, const void*>, int> g_smem_limit;
 std::map<unsigned long long, int> g_capturing;
 std::vector<Launch> g_launches;
 int g_device = 0, g_set_attribute_calls = 0;
+int g_word = 0, g_unfinished = 0;  // what a copy of 4 bytes to the host brings; fills that nobody has waited for
 void (*g_on_smem_limit)() = nullptr;
 cudaError_t g_last = cudaSuccess;
 dim3 g_push_grid, g_push_block;
@@ -62,6 +63,9 @@ int fake_launch(int i, char* name, int size, int* grid3, long long* smem) {
   *smem = static_cast<long long>(l.smem);
   return l.device;
 }
+
+void fake_set_word(int w) { g_word = w; }
+int fake_unfinished() { return g_unfinished; }
 
 // ---- what the compiler's host code calls
 void** __cudaRegisterFatBinary(void*) {
@@ -142,9 +146,18 @@ cudaError_t cudaGetLastError() {
   g_last = cudaSuccess;
   return e;
 }
-cudaError_t cudaDeviceSynchronize() { return cudaSuccess; }
-cudaError_t cudaMemcpy(void*, const void*, size_t, cudaMemcpyKind) { return cudaSuccess; }
+cudaError_t cudaDeviceSynchronize() {
+  g_unfinished = 0;
+  return cudaSuccess;
+}
+cudaError_t cudaMemcpy(void* to, const void*, size_t n, cudaMemcpyKind kind) {
+  if (kind == cudaMemcpyDeviceToHost && n == 4) memcpy(to, &g_word, 4);
+  return cudaSuccess;
+}
 cudaError_t cudaMemcpyAsync(void*, const void*, size_t, cudaMemcpyKind, cudaStream_t) { return cudaSuccess; }
-cudaError_t cudaMemset(void*, int, size_t) { return cudaSuccess; }
+cudaError_t cudaMemset(void*, int, size_t) {  // (of device memory: the host does not wait for it)
+  ++g_unfinished;
+  return cudaSuccess;
+}
 cudaError_t cudaMemsetAsync(void*, int, size_t, cudaStream_t) { return cudaSuccess; }
 }

@@ -148,3 +148,30 @@ def test_forwards_of_short_lists_share_no_scratch(lib):
     from paper_2609_34606_b200 import hsa
     sizes = {hsa.hsa_query_sizes(hsa.hsa_config(2, 128, 64, 300, 4680, k, 1, 0, 0.0, 0)).workspace for k in (1, 47, 48, 256)}
     assert len(sizes) == 1
+
+
+def cache8(lib, **kw):
+    """A context of the 8-bit cache over made-up device addresses."""
+    from paper_2609_34606_b200 import hsa
+    cfg = {**dict(num_heads=8, num_kv_heads=2, head_dim=128, page_tokens=64, max_pages=16, max_blocks=8, max_batch=4, max_tokens=512,
+                  softmax_scale=0.0, flags=0), **kw}
+    ctx = C.c_void_p()
+    bufs = hsa.hsa_kv8_buffers(*[i << 28 for i in range(1, 8)])
+    assert lib.hsa_kv8_create(C.byref(ctx), C.byref(hsa.hsa_kv8_config(*cfg.values())), C.byref(bufs)) == 0
+    return ctx
+
+
+def test_status_calls_return_when_what_they_clear_is_clear(lib):
+    """A fill of device memory runs behind the host's back, unordered with other streams: what is launched on one of them
+    after the call must find it done."""
+    ctx, ctx8 = Context(lib, 2, 128, 300, 300, n=300 * 64), cache8(lib)
+    assert lib.fake_unfinished() == 0        # (creation)
+    status, count = C.c_int32(), C.c_int64()
+    for word in (-5, -6, 0):
+        lib.fake_set_word(word)
+        assert lib.hsa_device_status(ctx.ctx, C.byref(status)) == 0 and status.value == word
+        assert lib.fake_unfinished() == 0
+        assert lib.hsa_kv8_device_status(ctx8, C.byref(status)) == 0 and status.value == word
+        assert lib.fake_unfinished() == 0
+    lib.fake_set_word(7)
+    assert lib.hsa_safe_pass_tiles(ctx.ctx, C.byref(count)) == 0 and count.value == 7 and lib.fake_unfinished() == 0
