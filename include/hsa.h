@@ -501,8 +501,15 @@ int hsa_kv8_attend(hsa_kv8* ctx, const void* q, int32_t n_tokens, int32_t batch,
                    int32_t causal, const int32_t* sel_idx_dev, const int32_t* sel_cnt_dev, int32_t max_topk, void* out,
                    int64_t out_tok_stride, int64_t out_head_stride, float* lse_dev, void* stream);
 
-/* Synchronises the device, reads and clears the status word: HSA_OK or a DEVICE_* code. */
+/* Synchronises the device, reads and clears the status word: HSA_OK or a DEVICE_* code (the first since the last read).
+ * After HSA_ERR_DEVICE_TIMEOUT the results of that attend call, and of those behind it up to this read, are undefined; the
+ * next one starts clean. */
 int hsa_kv8_device_status(hsa_kv8* ctx, int32_t* status_out);
+
+/* Bound, in nanoseconds, of each wait inside hsa_kv8_attend (for its own copies, products and warps; no CTA waits for
+ * another; default 2e9).  When one runs out the kernel ends without anything in flight and leaves
+ * HSA_ERR_DEVICE_TIMEOUT.  1..2.5e9, from 20,000 on in steps of that.  Calls that are made, or captured, from here on take it. */
+int hsa_kv8_set_wait_limit_ns(hsa_kv8* ctx, uint64_t wait_ns);
 
 /* Last CUDA error code recorded by a failing call on this context (0 if none). */
 int hsa_kv8_last_cuda_error(hsa_kv8* ctx);

@@ -13,6 +13,7 @@ namespace hsa {
 constexpr int kScaleMin = -48, kScaleMax = 52;
 constexpr float kTop8 = 1.152921504606846976e18f;  // 2^60, the largest magnitude that is stored
 constexpr int kDevNonfinite = HSA_ERR_DEVICE_NONFINITE;
+constexpr uint32_t kMaxPolls = 1u << 17, kPollNs = 20000;  // polls of a barrier before a wait runs out, and what one may sleep
 
 // The rows of each sequence in a call's tensors
 struct Kv8Rows {
@@ -94,6 +95,8 @@ struct Kv8Work {
   float* parts;        // [2 * CTAs][slot_floats]
   int64_t slot_floats;
   int32_t* tickets;    // [2 * CTAs], zero between calls
+  uint32_t first_try;  // where the count of a wait's polls begins: 0, or a later one for less patience
+  uint32_t look;       // cycles that a wait looks for, where that is less than a poll's sleep; else 0
 };
 
 int kv8_decode_rows(int D);                                   // rows up to which the kernel for few rows takes a call

@@ -16,6 +16,7 @@ struct hsa_kv8 {
   int dev, nsm;
   CUtensorMap tm_k, tm_v;
   int last_cuda_error;
+  uint64_t wait_ns;  // bound of the attention kernels' waits
 };
 
 namespace {
@@ -124,6 +125,7 @@ int hsa_kv8_create(hsa_kv8** out, const hsa_kv8_config* cfg, const hsa_kv8_buffe
   ctx->dev = dev;
   ctx->nsm = nsm;
   ctx->last_cuda_error = 0;
+  ctx->wait_ns = 2'000'000'000;
   cudaError_t e = cudaMemset(b->workspace, 0, kStatusBytes + kTicketBytes);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e == cudaSuccess) e = kv8_append_init(cfg->head_dim);
@@ -213,6 +215,8 @@ int hsa_kv8_attend(hsa_kv8* ctx, const void* q, int32_t n_tokens, int32_t batch,
   Kv8Work w{};
   w.tickets = reinterpret_cast<int32_t*>(ws + kStatusBytes);
   w.parts = reinterpret_cast<float*>(ws + kStatusBytes + kTicketBytes);
+  w.look = ctx->wait_ns < kPollNs ? static_cast<uint32_t>(2 * ctx->wait_ns) : 0;  // (at 2 GHz)
+  w.first_try = w.look ? 0 : kMaxPolls - static_cast<uint32_t>(ctx->wait_ns / kPollNs);
   const int ctas = ctx->nsm < kMaxCtas ? ctx->nsm : kMaxCtas;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = static_cast<int64_t>(max_q) * a.group <= kv8_decode_rows(c.head_dim)
@@ -230,6 +234,12 @@ int hsa_kv8_device_status(hsa_kv8* ctx, int32_t* status_out) {
   if (e == cudaSuccess && v != 0) e = cudaDeviceSynchronize();  // (the fill is not ordered with what other streams are given next)
   if (e != cudaSuccess) return cuda_fail(ctx, e);
   *status_out = v;
+  return HSA_OK;
+}
+
+int hsa_kv8_set_wait_limit_ns(hsa_kv8* ctx, uint64_t wait_ns) {
+  if (!ctx || wait_ns == 0 || wait_ns > 2'500'000'000) return HSA_ERR_INVALID_ARG;
+  ctx->wait_ns = wait_ns;
   return HSA_OK;
 }
 

@@ -276,7 +276,8 @@ __device__ __noinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work& w
   if (a.lse && d0 == 0) a.lse[lse_at] = ref.lse(l);
 }
 
-template <int D>
+// LOOK: waits of less than a poll's sleep
+template <int D, bool LOOK>
 __global__ void __launch_bounds__(kThreads, 1)
 kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant__ Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using Smem = ChunkSmem<D>;
@@ -319,11 +320,11 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
   Kv8Walk walk;
-  uint32_t tries = 0;
-  bool ok = true;  // false: a wait ran out; nothing more is waited for
+  uint32_t tries = w.first_try;
+  bool ok = true;  // false: a wait ran out; nothing more is waited for or handed on
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    tries = mbar_poll(bar, parity, tries);
-    return ok = tries == 0;
+    tries = LOOK ? mbar_look(bar, parity, tries, w.look) : mbar_poll(bar, parity, tries);
+    return ok = tries != kMaxPolls;
   };
   // the same for a whole warp that stays together
   const auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
@@ -336,7 +337,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 0) {
       // ---- loads.  The lanes look up 32 pages at once.
-      uint32_t n = 0;
+      uint32_t n = 0, ahead = 0;  // pages; 1: keys whose values have not been asked for
       while (ok && walk.next(a, w, sm.plan)) {
         const Kv8Item& it = walk.g.it;
         const int per = shared_rows(it) ? 2 : 1, s1 = walk.g.s1 * per;  // pages
@@ -366,8 +367,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm.k_full[st]);
             if (!warp_wait(&sm.vc_empty[sv], ((n / kVStages) & 1) ^ 1)) {
-              if (lane == 0) mbar_arrive(&sm.vc_full[sv]);
-              ++n;
+              ahead = 1;
               break;
             }
             if (elect_one_sync()) {
@@ -382,9 +382,12 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           }
         }
       }
-      if (!ok) {  // pages that nobody took: their loads must not outlive the CTA
-        for (uint32_t i = 1; i <= kKStages && i <= n; ++i) mbar_poll(&sm.k_full[(n - i) % kKStages], ((n - i) / kKStages) & 1, 0);
-        for (uint32_t i = 1; i <= kVStages && i <= n; ++i) mbar_poll(&sm.vc_full[(n - i) % kVStages], ((n - i) / kVStages) & 1, 0);
+      // the last pages, a lane each, whether somebody takes them or not
+      static_assert(kKStages <= 16 && kVStages <= 16);
+      const uint32_t back = lane % 16 + 1, all = lane < 16 ? n + ahead : n, ring = lane < 16 ? kKStages : kVStages;
+      if (back <= ring && back <= all) {
+        const uint32_t i = all - back;
+        if (!mbar_drain(lane < 16 ? &sm.k_full[i % kKStages] : &sm.vc_full[i % kVStages], (i / ring) & 1)) ok = false;
       }
     } else if (warp <= 2) {
       // ---- products of a tile.  A unit is a page of the item (of shared rows: every other page); scores are two units ahead, and
@@ -406,7 +409,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         };
         const auto scores = [&]() {
           const uint32_t k = k0 + st * (kPage / 16), d = s0 + (ns & 1) * 128, b = (ns & 1) * 2 + t;
-          if (elect_one_sync()) {
+          if (elect_one_sync() && ok) {
 #pragma unroll
             for (int term = 0; term < 2; ++term)
 #pragma unroll
@@ -433,7 +436,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
           const uint32_t sv = nv % kBStages, v = v0 + sv * (kPage * 2 / 16), b = (n & 1) * 2 + t, pw = s0 + (n & 1) * 128;
           wait(&sm.p_full[b], (n / 2) & 1);
           tc_fence_after();
-          if (elect_one_sync()) {
+          if (elect_one_sync() && ok) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) tc_mma_ts_lo(o0, pw + kk * 8, v + kk * 128, hi_v, id_o, u > 0 || kk > 0);
             tc_commit(&sm.pv_done[b]);
@@ -452,7 +455,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       }
       if (elect_one_sync()) tc_commit(&sm.done[t]);
       __syncwarp();
-      if (mbar_poll(&sm.done[t], 0, 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
+      if (!mbar_drain(&sm.done[t], 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
     } else {
       // ---- looks ahead for warps 1 and 2, who would otherwise poll three barriers for a page (each some 250 cycles beside busy
       // warps): arrives with the weights of a page where its values and the keys of the scores behind it are there.  Where the
@@ -460,7 +463,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       uint32_t n = 0, ks = 0, kr = 0, nv = 0;  // units of a tile before the item; stage of K, rounds; pages of V
       const auto keys = [&](bool same) {
         wait(&sm.k_full[ks], kr & 1);
-        mbar_arrive_if(&sm.k_empty[ks], same && lane == 0);
+        mbar_arrive_if(&sm.k_empty[ks], same && lane == 0 && ok);
         ++ks;
         kr += ks == kKStages;
         ks = ks == kKStages ? 0 : ks;
@@ -472,13 +475,13 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
 #pragma unroll 1
         for (int m = 0; m < pages; ++m, ++nv) {
           wait(&sm.vb_full[nv % kBStages], (nv / kBStages) & 1);
-          mbar_arrive_if(&sm.vb_empty[nv % kBStages], same && lane == 0);
+          mbar_arrive_if(&sm.vb_empty[nv % kBStages], same && lane == 0 && ok);
           if (m + first < pages) keys(same);
           const uint32_t at = n + (same ? m / 2 : m), b = (at & 1) * 2;
           for (int t = 0; t < 2; ++t) {
             if (same && t != (m & 1)) continue;
             if (at >= 2) wait(&sm.p_full[b + t], (at / 2 + 1) & 1);  // (the weights before these are complete)
-            mbar_arrive_if(&sm.p_full[b + t], lane == 0);
+            mbar_arrive_if(&sm.p_full[b + t], lane == 0 && ok);
           }
         }
         n += walk.g.s1 - walk.g.s0;
@@ -512,8 +515,8 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         }
         fence_proxy_async_smem();
         __syncwarp();
-        mbar_arrive_if(&sm.vb_full[b], lane == 0);
-        mbar_arrive_if(&sm.vc_empty[sv], lane == 0);
+        mbar_arrive_if(&sm.vb_full[b], lane == 0 && ok);
+        mbar_arrive_if(&sm.vc_empty[sv], lane == 0 && ok);
       }
     }
   } else {
@@ -542,7 +545,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
       if (lane >= lo && lane < hi) sm.qscale[row] = e * a.scale_log2;
       fence_proxy_async_smem();
       __syncwarp();
-      mbar_arrive_if(&sm.q_full, lane == 0);
+      mbar_arrive_if(&sm.q_full, lane == 0 && ok);
       if (same) {
         wait(&sm.q_full, items & 1);
         __syncwarp();
@@ -618,7 +621,7 @@ kv8_chunk_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant_
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
-        mbar_arrive_if(&sm.p_full[b], lane == 0);
+        mbar_arrive_if(&sm.p_full[b], lane == 0 && ok);
       }
       kn += units * (same ? 2 : 1);
       wait(&sm.pv_done[((n - 1) & 1) * 2 + t], ((n - 1) / 2) & 1);
@@ -796,14 +799,19 @@ constexpr size_t smem_bytes() {
   static_assert(sizeof(ChunkSmem<D>) + 1024 <= 232448, "shared memory of an SM");
   return sizeof(ChunkSmem<D>) + 1024;
 }
+using ChunkKernel = void (*)(Kv8AttendArgs, Kv8Work, CUtensorMap, CUtensorMap);
+ChunkKernel kernel_of(int D, bool look) {
+  return D == 128 ? look ? kv8_chunk_kernel<128, true> : kv8_chunk_kernel<128, false> : look ? kv8_chunk_kernel<64, true> : kv8_chunk_kernel<64, false>;
+}
 
 }  // namespace
 
 size_t kv8_chunk_slot(int D) { return static_cast<size_t>(2 * kTile) * (D + 3); }
 
 cudaError_t kv8_chunk_init(int D) {
-  return D == 128 ? cudaFuncSetAttribute(kv8_chunk_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<128>()))
-                  : cudaFuncSetAttribute(kv8_chunk_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<64>()));
+  const int bytes = static_cast<int>(D == 128 ? smem_bytes<128>() : smem_bytes<64>());
+  const cudaError_t e = cudaFuncSetAttribute(kernel_of(D, false), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  return e == cudaSuccess ? cudaFuncSetAttribute(kernel_of(D, true), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : e;
 }
 
 cudaError_t launch_kv8_chunk(const Kv8AttendArgs& a, Kv8Work w, int D, int ctas, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
@@ -827,7 +835,7 @@ cudaError_t launch_kv8_chunk(const Kv8AttendArgs& a, Kv8Work w, int D, int ctas,
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, D == 128 ? kv8_chunk_kernel<128> : kv8_chunk_kernel<64>, a, w, tm_k, tm_v);
+  return cudaLaunchKernelEx(&cfg, kernel_of(D, w.look != 0), a, w, tm_k, tm_v);
 }
 
 }  // namespace hsa

@@ -72,7 +72,6 @@ struct DecodeSmem {
   uint64_t k_full[Sh::kStages], v_full[Sh::kStages], empty[Sh::kStages];
   uint64_t s_full[2], s_free[2], p_full[2], p_free[2], q_full[2], q_free[2], other_full, other_free, done[2];
   uint32_t tmem;
-  int last;
   Kv8Plan plan;
 };
 
@@ -227,7 +226,8 @@ __device__ __forceinline__ void join_parts(const Kv8AttendArgs& a, const Kv8Work
   }
 }
 
-template <int D, int R>
+// LOOK: waits of less than a poll's sleep
+template <int D, int R, bool LOOK>
 __global__ void __launch_bounds__((DecodeShape<D, R>::kThreads), 1)
 kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant__ Kv8Work w, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   using Sh = DecodeShape<D, R>;
@@ -267,11 +267,11 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
   Kv8Walk walk;
-  uint32_t tries = 0;
-  bool ok = true;  // false: a wait ran out; nothing more is waited for
+  uint32_t tries = w.first_try;
+  bool ok = true;  // false: a wait ran out; nothing more is waited for or handed on
   const auto wait = [&](uint64_t* bar, uint32_t parity) {
-    tries = mbar_poll(bar, parity, tries);
-    return ok = tries == 0;
+    tries = LOOK ? mbar_look(bar, parity, tries, w.look) : mbar_poll(bar, parity, tries);
+    return ok = tries != kMaxPolls;
   };
   // the same for a whole warp that stays together
   const auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return ok = __all_sync(0xffffffffu, wait(bar, parity)); };
@@ -324,11 +324,13 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         }
       }
     }
-    if (!ok)  // pages that nobody took: their loads must not outlive the CTA
-      for (uint32_t i = 1; i <= kStages && i <= n; ++i) {
-        mbar_poll(&sm.k_full[(n - i) % kStages], ((n - i) / kStages) & 1, 0);
-        mbar_poll(&sm.v_full[(n - i) % kStages], ((n - i) / kStages) & 1, 0);
-      }
+    // the last pages, a lane each, whether somebody takes them or not
+    static_assert(kStages <= 16);
+    const uint32_t back = lane % 16 + 1;
+    if (back <= kStages && back <= n) {
+      const uint32_t st = (n - back) % kStages;
+      if (!mbar_drain(lane < 16 ? &sm.k_full[st] : &sm.v_full[st], ((n - back) / kStages) & 1)) ok = false;
+    }
   } else if (warp == 1) {
     // ---- first products.  (The warps that issue products stay together and choose a lane at the last moment, so that the operands
     // are in uniform registers.)
@@ -344,7 +346,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         wait(&sm.k_full[st], round & 1);
         wait(&sm.s_free[b], ((n / 2) & 1) ^ 1);
         tc_fence_after();
-        if (elect_one_sync()) {
+        if (elect_one_sync() && ok) {
 #pragma unroll
           for (int kk = 0; kk < D / 32; ++kk)  // (descriptors count in 16 bytes)
             mma_f8_lo(tm + Sh::kS + b * N, k + kk * 2, q + kk * 2, row_desc_hi<D>(), row_desc_hi<D>(), id, kk > 0);
@@ -361,7 +363,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
     }
     if (elect_one_sync()) tc_commit(&sm.done[0]);
     __syncwarp();
-    if (mbar_poll(&sm.done[0], 0, 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
+    if (!mbar_drain(&sm.done[0], 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
   } else if (warp == 3) {
     // ---- second products, a page at a time (of pages that are not there too: nobody looks at what they give)
     constexpr uint32_t id = idesc_e4m3(128, NP, 1, 0) | 1u << 10;  // (B: e5m2)
@@ -378,7 +380,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         wait(&sm.v_full[st], round & 1);
         wait(&sm.p_full[b], (n / 2) & 1);
         tc_fence_after();
-        if (elect_one_sync()) {
+        if (elect_one_sync() && ok) {
 #pragma unroll
           for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
@@ -397,7 +399,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
     }
     if (elect_one_sync()) tc_commit(&sm.done[1]);
     __syncwarp();
-    if (mbar_poll(&sm.done[1], 0, 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
+    if (!mbar_drain(&sm.done[1], 0)) ok = false;  // (whatever ran out before: products in flight must not outlive the CTA)
   } else if (warp == 2) {
     // ---- rows of Q, an item ahead: a thread takes 8 dims of a row
     uint32_t items = 0;
@@ -487,12 +489,10 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
           const float vs = pg ? vs1 : vs0;
-          if (vs > 0.f) {
-            float x[R];
-            tmem_load_terms<R>(tmem + lanes + Sh::kO + ((i & 1) * 2 + pg) * NP, x);
+          float x[R];
+          tmem_load_terms<R>(tmem + lanes + Sh::kO + ((i & 1) * 2 + pg) * NP, x);
 #pragma unroll
-            for (int r = 0; r < R; ++r) o[r] = fmaf(x[r], vs, o[r]);
-          }
+          for (int r = 0; r < R; ++r) o[r] = vs > 0.f ? fmaf(x[r], vs, o[r]) : o[r];  // (0: a page that is not there)
         }
         tc_fence_before();
         added = i + kGroups;
@@ -527,7 +527,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
         }
         const float vs0_now = sm.meta[st][0].vs, vs1_now = sm.meta[st][1].vs;
         tc_fence_before();
-        mbar_arrive(&sm.s_free[b]);
+        mbar_arrive_if(&sm.s_free[b], ok);
         if (__builtin_expect(group_any(group, over), 0)) {
           // the maxima anew
           if (added < j) add(added);
@@ -565,11 +565,11 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
           }
         }
         fence_proxy_async_smem();
-        mbar_arrive(&sm.p_full[b]);
+        mbar_arrive_if(&sm.p_full[b], ok);
         vs0 = vs0_now;
         vs1 = vs1_now;
       }
-      if (lane == 0) mbar_arrive(&sm.q_free[qb]);
+      mbar_arrive_if(&sm.q_free[qb], ok && lane == 0);
       if (!writes && !both) continue;  // the item's one step was the other group's
 
       // ---- the item's sums: of weights over the keys, then a dim of every row
@@ -597,7 +597,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
               sm.other[R * D + R + r] = l[r];
             }
           }
-          mbar_arrive(&sm.other_full);
+          mbar_arrive_if(&sm.other_full, ok);
         } else {
           wait(&sm.other_full, merges & 1);
 #pragma unroll
@@ -608,7 +608,7 @@ kv8_decode_kernel(const __grid_constant__ Kv8AttendArgs a, const __grid_constant
             l[r] = fmaf(sm.other[R * D + R + r], k, l[r] * c);
             ref[r] = to;
           }
-          mbar_arrive(&sm.other_free);
+          mbar_arrive_if(&sm.other_free, ok);
         }
         ++merges;
       }
@@ -673,11 +673,11 @@ constexpr size_t smem_bytes() {
   static_assert(sizeof(DecodeSmem<D, R>) + 1024 <= 232448, "shared memory of an SM");
   return sizeof(DecodeSmem<D, R>) + 1024;
 }
-template <int D, int R>
+template <int D, int R, bool LOOK = false>
 cudaError_t init_one() {
-  return cudaFuncSetAttribute(kv8_decode_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<D, R>()));
+  return cudaFuncSetAttribute(kv8_decode_kernel<D, R, LOOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<D, R>()));
 }
-template <int D, int R>
+template <int D, int R, bool LOOK = false>
 cudaError_t launch_one(const Kv8AttendArgs& a, Kv8Work w, int64_t rows, int ctas, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                        cudaStream_t st) {
   w.tile_rows = R;
@@ -698,11 +698,12 @@ cudaError_t launch_one(const Kv8AttendArgs& a, Kv8Work w, int64_t rows, int ctas
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kv8_decode_kernel<D, R>, a, w, tm_k, tm_v);
+  return cudaLaunchKernelEx(&cfg, kv8_decode_kernel<D, R, LOOK>, a, w, tm_k, tm_v);
 }
 template <int D>
 cudaError_t launch_dim(const Kv8AttendArgs& a, const Kv8Work& w, int ctas, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t st) {
   const int64_t rows = static_cast<int64_t>(a.rows.max_rows) * a.group;
+  if (w.look) return launch_one<D, 16, true>(a, w, rows, ctas, tm_k, tm_v, st);
   return rows <= 2    ? launch_one<D, 2>(a, w, rows, ctas, tm_k, tm_v, st)
          : rows <= 4  ? launch_one<D, 4>(a, w, rows, ctas, tm_k, tm_v, st)
          : rows <= 8  ? launch_one<D, 8>(a, w, rows, ctas, tm_k, tm_v, st)
@@ -719,6 +720,7 @@ cudaError_t kv8_decode_init(int D) {
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 4>() : init_one<64, 4>();
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 8>() : init_one<64, 8>();
   if (e == cudaSuccess) e = D == 128 ? init_one<128, 16>() : init_one<64, 16>();
+  if (e == cudaSuccess) e = D == 128 ? init_one<128, 16, true>() : init_one<64, 16, true>();
   return e;
 }
 

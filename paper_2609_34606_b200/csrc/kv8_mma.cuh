@@ -21,10 +21,13 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 // mbar_wait in a handful of instructions: the roles of these kernels share the instruction caches of their SM, and the
-// unrolled loop, at every wait, costs more than the waits do.  `tries` is how many polls have been spent without success: 0, or,
-// after a wait that ran out, kMaxPolls, with which this one and all later ones give up at once.  Returns the new one.
-// (a poll may sleep for some 20 us: without that the waiting warps' polls take issue slots from the others)
-constexpr uint32_t kMaxPolls = 1u << 17;
+// unrolled loop, at every wait, costs more than the waits do.  `tries` is where the count of polls begins, or, after a wait that ran
+// out, kMaxPolls, with which all later ones give up at once.  Returns the new one.  A poll may sleep for some 20 us (without that
+// the waiting warps' polls take issue slots from the others).
+//
+// A thread whose wait ran out goes on, because its warp and others meet it at barriers of the CTA, but hands nothing on: it neither
+// arrives at an mbarrier nor issues a product, so that those behind it run out too, and no place is given back to the loads whose
+// last copy may still be in flight.  (A word in shared memory that the loads look at instead: 1437 us for a chunk of 1345.)
 __device__ __forceinline__ uint32_t mbar_poll(uint64_t* bar, uint32_t parity, uint32_t tries) {
   uint32_t after;
   asm volatile(
@@ -45,6 +48,16 @@ __device__ __forceinline__ uint32_t mbar_poll(uint64_t* bar, uint32_t parity, ui
       : "r"(smem_u32(bar)), "r"(parity), "r"(tries), "n"(kMaxPolls)
       : "memory");
   return after;
+}
+// What is in flight at the end (copies, products) is waited for with all patience, whatever ran out before: it must not outlive the CTA.
+__device__ __forceinline__ bool mbar_drain(uint64_t* bar, uint32_t parity) { return mbar_poll(bar, parity, 0) == 0; }
+// The same for a bound below a poll's sleep: looks for that many cycles.  (In instances of their own: a look ahead of the polls takes
+// 2 % of a chunk.)
+__device__ __forceinline__ uint32_t mbar_look(uint64_t* bar, uint32_t parity, uint32_t tries, uint32_t cycles) {
+  const uint32_t t0 = static_cast<uint32_t>(clock64());
+  while (tries != kMaxPolls && !mbar_test_wait(bar, parity))
+    if (static_cast<uint32_t>(clock64()) - t0 >= cycles) tries = kMaxPolls;
+  return tries;
 }
 // an arrival by some threads or sometimes, without a branch
 __device__ __forceinline__ void mbar_arrive_if(uint64_t* bar, bool yes) {

@@ -54,7 +54,7 @@ EXPORTS = [
     "hsa_destroy", "hsa_status_string",
     "hsa_rope_table", "hsa_rope",
     "hsa_kv8_query_sizes", "hsa_kv8_create", "hsa_kv8_append", "hsa_kv8_attend", "hsa_kv8_device_status",
-    "hsa_kv8_last_cuda_error", "hsa_kv8_destroy",
+    "hsa_kv8_set_wait_limit_ns", "hsa_kv8_last_cuda_error", "hsa_kv8_destroy",
 ]
 
 
@@ -153,6 +153,7 @@ def _load() -> C.CDLL:
     lib.hsa_kv8_append.argtypes = [vp, vp, vp, i32, i32, i64, i64, vp, i32, vp, C.POINTER(hsa_rope_args), vp]
     lib.hsa_kv8_attend.argtypes = [vp, vp, i32, i32, i64, i64, vp, i32, vp, i32, vp, vp, i32, vp, i64, i64, vp, vp]
     lib.hsa_kv8_device_status.argtypes = [vp, C.POINTER(i32)]
+    lib.hsa_kv8_set_wait_limit_ns.argtypes = [vp, C.c_uint64]
     lib.hsa_kv8_last_cuda_error.argtypes = [vp]
     lib.hsa_kv8_destroy.argtypes = [vp]
     for name in EXPORTS:
@@ -425,6 +426,10 @@ def hsa_kv8_device_status(ctx: int) -> int:
     s = C.c_int32()
     _check(_lib.hsa_kv8_device_status(ctx, C.byref(s)), "hsa_kv8_device_status")
     return s.value
+
+
+def hsa_kv8_set_wait_limit_ns(ctx: int, wait_ns: int) -> None:
+    _check(_lib.hsa_kv8_set_wait_limit_ns(ctx, int(wait_ns)), "hsa_kv8_set_wait_limit_ns")
 
 
 def hsa_kv8_last_cuda_error(ctx: int) -> int:
@@ -772,6 +777,9 @@ class KV8Cache:
 
     def device_status(self) -> int:
         return hsa_kv8_device_status(self.ctx)
+
+    def set_wait_limit_ns(self, wait_ns: int) -> None:
+        hsa_kv8_set_wait_limit_ns(self.ctx, wait_ns)
 
     def destroy(self) -> None:
         if getattr(self, "ctx", None):

@@ -175,3 +175,12 @@ def test_status_calls_return_when_what_they_clear_is_clear(lib):
         assert lib.fake_unfinished() == 0
     lib.fake_set_word(7)
     assert lib.hsa_safe_pass_tiles(ctx.ctx, C.byref(count)) == 0 and count.value == 7 and lib.fake_unfinished() == 0
+
+
+def test_wait_limit_of_the_8_bit_cache(lib):
+    ctx, ns = cache8(lib), C.c_uint64
+    assert lib.hsa_kv8_set_wait_limit_ns(None, ns(1)) == -1
+    for bad in (0, 2_500_000_001, (1 << 64) - 1):
+        assert lib.hsa_kv8_set_wait_limit_ns(ctx, ns(bad)) == -1
+    for good in (1, 19_999, 20_001, 2_500_000_000):
+        assert lib.hsa_kv8_set_wait_limit_ns(ctx, ns(good)) == 0
