@@ -621,6 +621,24 @@ _SCALINGS = {"none": HSA_ROPE_SCALE_NONE, "linear": HSA_ROPE_SCALE_LINEAR, "base
              "bands": HSA_ROPE_SCALE_BANDS}
 
 
+class _Rotate(torch.autograd.Function):
+    """The rotation with its gradient, which is the transposed one (whose own is the rotation again)."""
+
+    @staticmethod
+    def forward(ctx, x, rope, positions, transpose):
+        ctx.rope, ctx.transpose = rope, transpose
+        ctx.save_for_backward(positions)
+        return rope._rotate(x, positions, transpose, x.new_empty(x.shape))
+
+    @staticmethod
+    def backward(ctx, grad):
+        # (a gradient comes with whatever strides and alignment it was made with, broadcast ones among them)
+        s, wide = grad.stride(), 16 // grad.element_size()
+        if s[2] != 1 or min(s) < 1 or s[0] < grad.shape[2] or s[1] < grad.shape[2] or s[0] % wide or s[1] % wide or grad.data_ptr() % 16:
+            grad = grad.clone(memory_format=torch.contiguous_format)
+        return _Rotate.apply(grad, ctx.rope, ctx.saved_tensors[0], not ctx.transpose), None, None, None
+
+
 class RotaryPositions:
     """Rotary positions of one layer: the frequency table on the device, and the calls that take it.
 
@@ -664,11 +682,17 @@ class RotaryPositions:
 
     def apply(self, x: torch.Tensor, positions: Optional[torch.Tensor] = None, transpose: bool = False,
               out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Rotates x [tokens, H, d]; transpose=True applies the transposed map, the gradient of the rotation."""
+        """Rotates x [tokens, H, d]; transpose=True applies the transposed map, the gradient of the rotation.  Where x requires
+        a gradient it is recorded (out= is refused then); positions must not change before the backward pass."""
         if x.dim() != 3 or x.shape[2] != self.head_dim or x.get_device() != self._index:
             raise ValueError(f"x: expected [tokens, H, {self.head_dim}] on {self.device}")
-        if out is None:
-            out = x.new_empty(x.shape)
+        if torch.is_grad_enabled() and (x.requires_grad or out is not None and out.requires_grad):
+            if out is not None:
+                raise ValueError("out: a result that is written in place records no gradient (use torch.no_grad)")
+            return _Rotate.apply(x, self, positions, transpose)
+        return self._rotate(x, positions, transpose, x.new_empty(x.shape) if out is None else out)
+
+    def _rotate(self, x: torch.Tensor, positions: Optional[torch.Tensor], transpose: bool, out: torch.Tensor) -> torch.Tensor:
         hsa_rope(x, out, self.args(positions, x.shape[0]), HSA_ROPE_TRANSPOSE if transpose else 0)
         return out
 
@@ -678,7 +702,7 @@ class KV8Cache:
 
     Buffers (attributes): k_codes, v_codes float8_e4m3fn [pages, kv heads, 64, d]; k_scale, v_scale fp32 [pages, kv heads];
     page_table int32 [batch, blocks], which the caller fills; ksum fp32 [batch, kv heads, blocks, d] where key_sums is
-    True (or the tensor itself)."""
+    True (or the tensor itself).  A cache is for serving: append and attend record no gradients."""
 
     def __init__(self, num_heads: int, num_kv_heads: int, head_dim: int, max_pages: int, max_blocks: int, max_batch: int = 1,
                  max_tokens: int = 1, softmax_scale: float = 0.0, device: str | torch.device = "cuda:0",
