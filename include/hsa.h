@@ -356,7 +356,9 @@ int hsa_destroy(hsa_ctx* ctx);
                                     frequency, the last is divided by s */
 #define HSA_ROPE_SCALE_BANDS 3   /* with r = trained_tokens * f / 2 pi turns over the trained context:
                                     g = clamp((r - beta_slow) / (beta_fast - beta_slow), 0, 1),
-                                    f (g + (1 - g) / s), amplitude 0.1 ln s + 1 */
+                                    f (g + (1 - g) / s), amplitude 0.1 ln s + 1.  The ramp is over turns, as published;
+                                    a ramp over the index of the pair between two borders, which other programs use,
+                                    gives other frequencies inside the band */
 typedef struct {
   int32_t head_dim;       /* a multiple of 8, 8..512                                            */
   int32_t rot_dim;        /* even, 2..head_dim                                                  */
@@ -371,7 +373,8 @@ typedef struct {
   double beta_slow;
 } hsa_rope_config;
 
-/* The table of a configuration, on the host: turns_host uint64[rot_dim / 2], amplitude_host one float. */
+/* The table of a configuration, on the host: turns_host uint64[rot_dim / 2], amplitude_host one float (the formula's: a
+ * caller whose model has another puts it into hsa_rope_args). */
 int hsa_rope_table(const hsa_rope_config* cfg, uint64_t* turns_host, float* amplitude_host);
 
 /* What a call needs of it.  positions_dev: device int32 [n_axes][tokens], axis_stride elements apart; NULL:

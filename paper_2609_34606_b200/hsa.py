@@ -13,6 +13,7 @@ takes device pointers; `HSAContext` bundles buffer allocation with them.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -646,12 +647,13 @@ class RotaryPositions:
     layout       "half": pairs (i, i + rot_dim / 2); "interleaved": pairs (2 i, 2 i + 1)
     axis_pairs   pairs of each position axis, 1 to 3 of them (default: one axis)
     scaling      "none", "linear", "base" or "bands" with `factor` (see hsa_rope_config)
+    amplitude    what rotated values are multiplied by (default: the scaling's, 0.1 ln factor + 1 for "bands", else 1)
     """
 
     def __init__(self, head_dim: int, rot_dim: Optional[int] = None, layout: str = "half", base: float = 10000.0,
                  axis_pairs: Optional[Sequence[int]] = None, scaling: str = "none", factor: float = 1.0,
                  trained_tokens: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0,
-                 device: str | torch.device = "cuda:0"):
+                 device: str | torch.device = "cuda:0", amplitude: Optional[float] = None):
         if layout not in _LAYOUTS or scaling not in _SCALINGS:
             raise ValueError(f"layout {layout!r} or scaling {scaling!r} unknown")
         rot_dim = head_dim if rot_dim is None else rot_dim
@@ -662,7 +664,11 @@ class RotaryPositions:
         axes = (C.c_int32 * 3)(*pairs, *[0] * (3 - len(pairs)))
         self.cfg = hsa_rope_config(head_dim, rot_dim, _LAYOUTS[layout], self.n_axes, axes, _SCALINGS[scaling], base, factor,
                                    trained_tokens, beta_fast, beta_slow)
-        turns, amplitude = hsa_rope_table(self.cfg)
+        turns, own_amplitude = hsa_rope_table(self.cfg)
+        amplitude = own_amplitude if amplitude is None else float(amplitude)
+        if not math.isfinite(amplitude):
+            raise ValueError("amplitude: expected a finite number")
+        self.amplitude = amplitude
         self.turns = turns.to(device)
         self.head_dim, self.device, self._index = head_dim, self.turns.device, self.turns.get_device()
         self._args = (rot_dim, _LAYOUTS[layout], self.n_axes, axes, amplitude, self.turns.data_ptr())
