@@ -34,3 +34,84 @@ def test_attention_that_gives_up_leaves_the_context_usable(cuda_device, d, Hq, H
     for _ in range(2):
         _, got, lse = c.attend(counts, True, sel=sel, q=q, check=False)
         assert c.cache.device_status() == 0 and torch.equal(got, want) and torch.equal(lse, want_lse)
+
+
+# (query heads, key heads, tokens of each sequence): rows of a key head up to 2, 4, 8 and 16, each instance full and not
+FEW = [(3, 3, [2, 1, 2]), (3, 1, [1, 1, 0]), (4, 4, [3, 4, 1]), (8, 1, [1, 1, 1]), (5, 1, [1, 0, 1]), (2, 2, [7, 8, 1]),
+       (16, 1, [1, 1, 1]), (9, 1, [1, 1, 0]), (8, 2, [4, 3, 2]), (4, 4, [16, 9, 12]), (5, 1, [3, 2, 1])]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,counts", FEW)
+def test_few_rows_of_every_instance(cuda_device, d, Hq, Hkv, counts):
+    """Against the reference: whole histories and lists, causal and not, parts of an item on several SMs, rows that see nothing."""
+    lengths = [16, 777, 5000]
+    c = Case(cuda_device, Hq, Hkv, d, lengths, seed=32, max_tokens=6000)
+    c.append(lengths, twin=False)
+    c.take_gpu_state()
+    rng = np.random.default_rng(4)
+    for causal in (True, False):
+        c.attend(counts, causal)
+        c.attend(counts, causal, sel=[[list(rng.permutation(-(-n // 64))[:1 + (3 * h) % 7]) for h in range(Hkv)] for n in lengths])
+        c.attend(counts, causal, sel=[[[]] * Hkv, [[12, 3, 3, 0]] * Hkv, [list(range(78, -1, -1))] * Hkv])
+        c.attend(counts, causal, lengths=[0, 1, max(0, counts[2] - 1)])
+    assert c.cache.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,most", [(2, 2, 1), (4, 2, 2), (4, 2, 4), (4, 2, 8), (6, 1, 2)])
+def test_few_rows_leave_other_rows_alone(cuda_device, d, Hq, Hkv, most):
+    """Rows behind the last sequence, between sequences and of sequences that do not fit stay as they were, those of lse too."""
+    c = Case(cuda_device, Hq, Hkv, d, [300, 300, 300], seed=33)
+    c.append([300, 300, 300], twin=False)
+    n, m = 5 * most, most
+    q = c.randn(n, Hq, d).to(cuda_device)
+    i32 = lambda x: dev_i32(x, cuda_device)
+    for starts, lengths, served in [([1, 1 + m, 1 + 2 * m, 1 + 3 * m], [300, 200, 100], [0, 1, 2]), ([0, 2 * m + 1, m, 3 * m], [300, 200, 100], []),
+                                    ([m, 2 * m, 3 * m, 5 * m + 1], [300, 200, 100], [0, 1]), ([0, m, 2 * m, 3 * m], [300, -1, 321], [0]),
+                                    ([-1, m - 1, m, 3 * m + 1], [300, 200, 100], [1])]:
+        out, lse = torch.full_like(q, 7.0), torch.full((n, Hq), 7.0, device=cuda_device)
+        hsa.hsa_kv8_attend(c.cache.ctx, q, 3, i32(starts), m, i32(lengths), True, None, None, out, lse)
+        assert c.cache.device_status() == (0 if len(served) == 3 else hsa.HSA_ERR_DEVICE_BOUNDS)
+        mine = torch.zeros(n, dtype=torch.bool, device=cuda_device)
+        for s in served:
+            mine[starts[s]:starts[s + 1]] = True
+        assert (out[~mine] == 7.0).all() and (lse[~mine] == 7.0).all()
+        assert (out[mine] != 7.0).any(-1).all() and (lse[mine] != 7.0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,counts", FEW)
+def test_few_rows_are_independent(cuda_device, d, Hq, Hkv, counts):
+    """A query that is not finite spoils its own row alone; pages outside the pools and entries outside the table are not seen;
+    twice the same call, the same bits, in a graph too."""
+    c = Case(cuda_device, Hq, Hkv, d, [400, 400, 9000], seed=34, max_tokens=10000)
+    c.append([400, 400, 9000], twin=False)
+    n = sum(counts)
+    q, want, want_lse = c.attend(counts, True, check=False)
+    bad = q.clone()
+    bad[0, Hq - 1, 3], bad[n - 1, 0, 0] = float("nan"), float("inf")
+    _, got, lse = c.attend(counts, True, q=bad, check=False)
+    keep = torch.ones(n, Hq, dtype=torch.bool)
+    keep[0, Hq - 1] = keep[n - 1, 0] = False
+    assert torch.equal(got.cpu()[keep], want.cpu()[keep]) and torch.equal(lse.cpu()[keep], want_lse.cpu()[keep])
+    assert got.cpu()[0, Hq - 1].isnan().all()
+    qd, starts, lengths, out = q.to(cuda_device), dev_i32(np.concatenate([[0], np.cumsum(counts)]), cuda_device), dev_i32(c.held, cuda_device), torch.empty_like(want)
+    call = lambda o, **kw: c.cache.attend(qd, lengths, token_start=starts, max_q=max(counts), out=o, **kw)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and c.cache.device_status() == 0
+    idx = torch.tensor([[[0, -1, 3, 141]], [[99999, 2, 1 << 30, 5]], [[7, 8, -5, 9]]], dtype=torch.int32, device=cuda_device).expand(3, Hkv, 4).contiguous()
+    cnt = torch.full((3, Hkv), 4, dtype=torch.int32, device=cuda_device)
+    call(out, sel_idx=idx, sel_cnt=cnt)
+    assert c.cache.device_status() == hsa.HSA_ERR_DEVICE_BOUNDS
+    good = torch.tensor([[[0, 3, 3]], [[2, 5, 5]], [[7, 8, 9]]], dtype=torch.int32, device=cuda_device).expand(3, Hkv, 3).contiguous()
+    only = call(torch.empty_like(out), sel_idx=good, sel_cnt=torch.tensor([[2] * Hkv, [2] * Hkv, [3] * Hkv], dtype=torch.int32, device=cuda_device))
+    # the same keys in other places of a step: fp32 sums in another order, a bf16 step apart at most
+    assert torch.allclose(out.float(), only.float(), atol=2.0 ** -12, rtol=2.0 ** -7) and c.cache.device_status() == 0
