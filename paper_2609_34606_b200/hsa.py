@@ -367,6 +367,7 @@ def hsa_destroy(ctx: int) -> None:
     _check(_lib.hsa_destroy(ctx), "hsa_destroy")
 
 
+_MOST = (1 << 31) - 1  # the library counts tokens in 32 bits, and ctypes cuts what is longer down to them
 _TYPES = {torch.bfloat16: HSA_TYPE_BF16, torch.float16: HSA_TYPE_FP16, torch.float32: HSA_TYPE_FP32}
 
 
@@ -384,6 +385,8 @@ def hsa_rope(x: torch.Tensor, out: torch.Tensor, rope: hsa_rope_args, flags: int
     if code is None or out.dtype != x.dtype:
         raise ValueError("hsa_rope: expected x and out of one type, bf16, fp16 or fp32")
     shape, s, o = x.shape, x.stride(), out.stride()
+    if shape[0] > _MOST:
+        raise ValueError("hsa_rope: more than 2^31 - 1 tokens")
     if len(shape) != 3 or out.shape != shape or not x.is_cuda or out.get_device() != x.get_device():
         raise ValueError("hsa_rope: expected CUDA tensors [tokens, H, d] of one shape")
     if s[2] != 1 or o[2] != 1:
@@ -761,6 +764,8 @@ class KV8Cache:
             raise ValueError("token_start: expected one entry more than there are sequences")
         _on_current(t, name)
         if most is not None:
+            if most > _MOST:
+                raise ValueError("max_new, max_q: more than 2^31 - 1 tokens")
             return int(most)
         return shape[0] if token_start is not None else shape[0] // max(1, counts.numel())
 
