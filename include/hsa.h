@@ -484,7 +484,9 @@ int hsa_kv8_append(hsa_kv8* ctx, const void* k, const void* v, int32_t n_tokens,
 
 /* out[i][h] = sum_j softmax_j(scale q[i][h] . k_j) v_j over the tokens j of query i's sequence that it sees.
  *   q, out           device bf16 [n_tokens][num_heads][head_dim], own strides each
- *   token_start_dev  as above: the queries of each sequence; max_q most of one sequence
+ *   token_start_dev  as above: the queries of each sequence
+ *   max_q            most rows of one sequence.  It chooses the kernel: up to 16 rows of a key head (max_q * num_heads /
+ *                    num_kv_heads) the one for few rows, whose rounding is its own
  *   lengths_dev      device int32[batch]: tokens each sequence holds, its queries' own tokens included
  *   causal           query i of n of a sequence of length L stands at L - n + i and sees the tokens up to itself;
  *                    0: all L

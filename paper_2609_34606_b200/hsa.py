@@ -773,7 +773,8 @@ class KV8Cache:
                max_new: Optional[int] = None, rope: Optional[RotaryPositions] = None,
                positions: Optional[torch.Tensor] = None) -> None:
         """Appends k, v [tokens, kv heads, d] behind the held[s] tokens of each sequence (int32 [batch]); token_start
-        int32 [batch + 1] where the sequences' rows differ in number, at most max_new to one.  Keys are rotated by
+        int32 [batch + 1] where the sequences' rows differ in number, at most max_new to one.  The launch is sized by
+        max_new: pass it with token_start (default there: all rows, as one sequence might have them).  Keys are rotated by
         `rope` at `positions` (default: their place in the sequence)."""
         most = self._rows(k, self.num_kv_heads, held, token_start, max_new, "k")
         if v.get_device() != self._index:
@@ -789,8 +790,11 @@ class KV8Cache:
                max_q: Optional[int] = None, causal: bool = True, sel_idx: Optional[torch.Tensor] = None,
                sel_cnt: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, with_lse: bool = False):
         """Attention of q [tokens, heads, d] over the lengths[s] tokens of each sequence (the queries' own included);
-        sel_idx int32 [batch, kv heads, n] with sel_cnt int32 [batch, kv heads]: block lists.  Returns out, or
-        (out, lse fp32 [tokens, heads]) with with_lse.  A row that belongs to no sequence is not written."""
+        sel_idx int32 [batch, kv heads, n] with sel_cnt int32 [batch, kv heads]: block lists.  max_q, the most rows of one
+        sequence, chooses the kernel (up to 16 rows of a key head: the one for few rows) and sizes the work: pass it with
+        token_start (default there: all rows, as one sequence might have them; 48 sequences of a token then take the kernel for
+        many rows).  Returns out, or (out, lse fp32 [tokens, heads]) with with_lse.  A row that belongs to no sequence is not
+        written."""
         most = self._rows(q, self.num_heads, lengths, token_start, max_q, "q")
         if (sel_idx is None) != (sel_cnt is None):
             raise ValueError("sel_idx and sel_cnt belong together")
