@@ -159,7 +159,9 @@ __device__ __forceinline__ void kv8_fill(const Kv8AttendArgs& a, const Kv8Work& 
   it->steps = max(1u, (static_cast<uint32_t>(it->pages) + (1u << log) - 1) >> log);
 }
 
-// (not inlined: a handful of places call it, seldom, and the kernels' roles share the instruction caches of an SM)
+// (Not inlined: the roles' walks call it, behind the segments of the plan, and they share the instruction caches of an SM.  So does
+// the plan of a launch with more items than threads, twice for each of a thread's items, empty ones too: one row of 49 sequences of
+// 8 key heads, 392 items of 384 threads, takes 50.7 us where 48 sequences take 48.0.)
 __device__ __noinline__ static Kv8Item kv8_item(const Kv8AttendArgs& a, const Kv8Work& w, int64_t i) {
   Kv8Item it;
   kv8_place(a, w, i, &it);

@@ -8,9 +8,9 @@
 // way, and serve all heads; a head's rows are loaded while those of the head before it are turned and rounded, in registers; and
 // one barrier a head does for the maxima of keys and values, the partners of the next head's half layout, and the sums of the last
 // head's keys.  (With four barriers a head and nothing in flight across them 31 us instead of 18 for 4680 tokens, 12 heads of 128.)
-// Measured: 4680 tokens, 12 heads of 128 with positions and sums, 43 MB: 18 us (2.5 TB/s: two CTAs to an SM, a start and three heads
-// each); 30,000 tokens of 8 heads without positions 36 us (5.1 TB/s), with them 60 (the rotation's instructions: the schedulers
-// issue two cycles of three); ragged prompts, heads of 64, 270 MB: 52 us (5.2 TB/s); a token of 48 sequences 5.9 us, of which the
+// Measured: 4680 tokens, 12 heads of 128 with positions and sums, 43 MB: 17 us (2.5 TB/s: 74 blocks in four groups of heads, two CTAs
+// to an SM, each with a start, the block's sines and three heads in turn); 30,000 tokens of 8 heads without positions 36 us (5.1 TB/s),
+// with them 59 (the rotation's instructions: the schedulers issue two cycles of three); ragged prompts, heads of 64, 270 MB: 52 us (5.2 TB/s); a token of 48 sequences 5.9 us, of which the
 // launch is 3 and the rest loads that wait for one another.
 #include <cuda_fp8.h>
 

@@ -29,8 +29,8 @@
 // The warps that issue products stay together and choose a lane for it at the last moment: so their operands are in uniform
 // registers.  A loop of one lane alone takes some 75 cycles to issue a product, beside busy warps, more than the product's 64.
 //
-// Measured: 4680 queries, 46,800 tokens, 12 heads of 128: 1160 us in a short run (1160 TFLOP/s), 1338 in a long one, at the
-// board's 1 kW (1005 TFLOP/s; a library product of bf16 alone holds 1373).  A page takes 1750 to 1900 cycles for both tiles: its
+// Measured: 4680 queries, 46,800 tokens, 12 heads of 128: 1160 to 1220 us in short runs (1160 to 1103 TFLOP/s), 1345 in a long one, at
+// the board's 1 kW (1000 TFLOP/s; a library product of bf16 alone holds 1373).  A page takes 1750 to 1900 cycles for both tiles: its
 // products 1280, its exponentials, of two warps on a special function unit at the same time, 1024.  What was tried and did not
 // help: turns at the exponentials (1192 us), an eighth or a quarter of them as polynomials (1185, 1196), half a row to a thread and
 // twice the warps (1400 against 1319), the next page's scores asked for early (1264 against 1237).

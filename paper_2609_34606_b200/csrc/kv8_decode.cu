@@ -27,8 +27,9 @@
 // together at an item's end; the group that had the item's last step writes it, while the other goes on.
 //
 // Measured: a token against 280,800 tokens of 12 heads of 128, 862 MB: 138 us, 6.25 TB/s (a plain copy: 6.54); a token of each of 48
-// sequences of 300 to 8000, four query heads to a key head, 233 MB: 50 us, 4.65 TB/s, where runs of unequal items begin and end
-// at different times; 777 tokens: 8.6 us, of which the launch is 3.  Up to 16 rows of a key head come here; with 32 the columns of
+// sequences of 300 to 8000, four query heads to a key head, 233 MB: 48 us, 4.85 TB/s, where runs of unequal items begin and end
+// at different times (sixteen rows of each: 86 us, of which the third term of the weights is 2); 777 tokens: 7.2 us, of which the
+// launch is 3.  Up to 16 rows of a key head come here; with 32 the columns of
 // both products and the registers of the softmax cost more than the kernel for many rows does (106 against 68 us for 8 sequences of
 // 9000 tokens).
 #include "kv8.cuh"
