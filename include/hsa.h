@@ -415,6 +415,9 @@ int hsa_rope(const void* x, void* out, int32_t type, int32_t n_tokens, int32_t n
  *     hsa_kv8_append   (keys, rotated on the way, and values -> pages; key sums)
  *     hsa_kv8_attend   (softmax attention over all blocks, or over those a selection names)
  *
+ * A page that a caller fills by other means has to be as an append leaves it: all 64 rows of finite codes, those behind the last token
+ * too (their weight is 0, but a NaN is a NaN), and scales that are powers of two, 2^-48..2^52.
+ *
  * The key sums have the layout that hsa_select_blocks_noalloc reads, so one sequence's lists can come from there.
  * Conventions as for hsa_ctx; calls of one context that are not ordered on the GPU must not overlap (they share
  * the workspace, and an append writes the pools). */
