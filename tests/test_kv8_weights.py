@@ -124,3 +124,26 @@ def test_scores_one_step_of_fp32_apart(cuda_device, d, Hq, Hkv, n, high, power):
     ref = reference(c, q, False)
     check(got, torch.from_numpy(ref[1]), ref, 0.0)
     assert (np.abs(lse.double().cpu().numpy() - ref[1]) <= 2.0 ** -22 * np.abs(ref[1])).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,n", ROWS)
+@pytest.mark.parametrize("tokens", [500, 9000])
+def test_rows_beside_far_ones_keep_their_bits(cuda_device, d, Hq, Hkv, n, tokens):
+    """Rows whose scores are ordinary give the same bits whether or not rows beside them have scores of 2^40."""
+    c = Case(cuda_device, Hq, Hkv, d, [tokens], seed=24, max_tokens=tokens)
+    k, v = c.randn(tokens, Hkv, d), c.randn(tokens, Hkv, d)
+    k[:, :, 0] = 0
+    k[70, :, 0], k[300, :, 0] = 2.0 ** 40, -2.0 ** 41
+    q = c.randn(n, Hq, d)
+    q[..., 0] = 0
+    far = torch.rand(n, Hq, generator=c.g) < 0.3
+    other = q.clone()
+    other[..., 0][far] = 1
+    c.append([tokens], k=k, v=v, twin=False)
+    _, want, want_lse = c.attend([n], True, q=q, check=False)
+    _, got, lse = c.attend([n], True, q=other, check=False)
+    keep = ~far
+    assert torch.equal(got.cpu()[keep], want.cpu()[keep]) and torch.equal(lse.cpu()[keep], want_lse.cpu()[keep])
+    assert not far.any() or (lse.cpu()[far] > 1e9).all()
+    assert c.cache.device_status() == 0
