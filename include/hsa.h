@@ -486,7 +486,8 @@ int hsa_kv8_append(hsa_kv8* ctx, const void* k, const void* v, int32_t n_tokens,
                    const hsa_rope_args* rope, void* stream);
 
 /* out[i][h] = sum_j softmax_j(scale q[i][h] . k_j) v_j over the tokens j of query i's sequence that it sees.
- *   q, out           device bf16 [n_tokens][num_heads][head_dim], own strides each
+ *   q, out           device bf16 [n_tokens][num_heads][head_dim], own strides each; out may be q with the same strides, and
+ *                    otherwise does not overlap it
  *   token_start_dev  as above: the queries of each sequence
  *   max_q            most rows of one sequence.  It chooses the kernel: up to 16 rows of a key head (max_q * num_heads /
  *                    num_kv_heads) the one for few rows, whose rounding is its own

@@ -115,3 +115,101 @@ def test_few_rows_are_independent(cuda_device, d, Hq, Hkv, counts):
     only = call(torch.empty_like(out), sel_idx=good, sel_cnt=torch.tensor([[2] * Hkv, [2] * Hkv, [3] * Hkv], dtype=torch.int32, device=cuda_device))
     # the same keys in other places of a step: fp32 sums in another order, a bf16 step apart at most
     assert torch.allclose(out.float(), only.float(), atol=2.0 ** -12, rtol=2.0 ** -7) and c.cache.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,n", [(128, 1), (128, 40), (64, 5)])
+def test_pages_behind_four_gigabytes(cuda_device, d, n):
+    """Pools of more than 2^32 bytes: pages at their far end give the bits that the same pages at the begin of small pools give."""
+    H, tokens = 12, 700
+    blocks, far = 11, (1 << 32) // (H * 64 * d) + 40
+    g = torch.Generator(device=cuda_device).manual_seed(51)
+    rand = lambda *s: torch.randn(*s, generator=g, device=cuda_device).to(torch.bfloat16)
+    k, v, q = rand(tokens, H, d), rand(tokens, H, d), rand(n, H, d)
+    rope = hsa.RotaryPositions(d, device=cuda_device)
+    res = []
+    for pages, table in ((blocks, torch.arange(blocks)), (far, far - 1 - torch.arange(blocks))):
+        c = hsa.KV8Cache(H, H, d, pages, blocks, 1, tokens, device=cuda_device, key_sums=True,
+                         page_table=table.to(torch.int32)[None].to(cuda_device))
+        c.append(k[:300], v[:300], dev_i32([0], cuda_device), rope=rope)
+        c.append(k[300:], v[300:], dev_i32([300], cuda_device), rope=rope)
+        out, lse = c.attend(q, dev_i32([tokens], cuda_device), with_lse=True)
+        assert c.device_status() == 0
+        at = table.to(cuda_device)
+        res.append([t.clone() for t in (c.k_codes.view(torch.uint8)[at], c.v_codes.view(torch.uint8)[at], c.k_scale[at], c.v_scale[at], c.ksum,
+                                        out, lse)])
+        c.destroy()
+        del c
+    assert all(torch.equal(x, y) for x, y in zip(*res))
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("counts", [[1, 1], [3, 1], [20, 100], [300, 260]])
+def test_heads_before_tokens_and_in_place(cuda_device, d, counts):
+    """Tensors that keep the tokens of a head together, results over the queries, and both."""
+    c, twin = (Case(cuda_device, 4, 2, d, [5000, 700], seed=52, max_tokens=6000) for _ in range(2))
+    k, v = c.append([5000, 700], twin=False)
+    flip = lambda t: t.to(cuda_device).transpose(0, 1).contiguous().transpose(0, 1)
+    held, starts = dev_i32([0, 0], cuda_device), dev_i32([0, 5000, 5700], cuda_device)
+    twin.cache.append(flip(k), flip(v), held, token_start=starts, max_new=5000)
+    pages = [p for _, _, p in c.written()]
+    for name in ("k_codes", "v_codes"):
+        a, b = (getattr(x.cache, name).view(torch.uint8)[pages] for x in (c, twin))
+        assert torch.equal(a, b), name
+    q, want, _ = c.attend(counts, True, check=False)
+    lengths, starts = dev_i32(c.held, cuda_device), dev_i32(np.concatenate([[0], np.cumsum(counts)]), cuda_device)
+    call = lambda x, out: c.cache.attend(x, lengths, token_start=starts, max_q=max(counts), out=out)
+    x = flip(q)
+    assert torch.equal(call(x, None), want) and torch.equal(call(x, torch.empty_like(x)), want)
+    assert call(x, x) is x and torch.equal(x, want)
+    y = q.to(cuda_device)
+    assert torch.equal(call(y, y), want) and c.cache.device_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hkv,d,n", [(4, 2, 128, 1), (2, 2, 64, 30)])
+def test_captured_step_follows_the_lengths(cuda_device, Hq, Hkv, d, n):
+    """Rotation, append and attention captured once; replays grow the sequences, whose lengths the graph itself counts up."""
+    steps, start = 70 if n == 1 else 8, [100, 64, 1]
+    room = [s + (steps + 2) * n for s in start]
+    eager, other = (Case(cuda_device, Hq, Hkv, d, room, seed=53, sums=True, max_tokens=1000) for _ in range(2))
+    g = torch.Generator().manual_seed(54)
+    past = [torch.randn(sum(start), Hkv, d, generator=g).to(torch.bfloat16) for _ in range(2)]
+    rope = hsa.RotaryPositions(d, device=cuda_device)
+    for c in (eager, other):
+        c.append(start, rope=rope, k=past[0], v=past[1], twin=False)
+    new = [torch.randn(steps, 3 * n, h, d, generator=g).to(torch.bfloat16).to(cuda_device) for h in (Hkv, Hkv, Hq)]
+    k, v, q = (torch.empty_like(t[0]) for t in new)
+    out, held = torch.empty_like(q), dev_i32(start, cuda_device)
+    pos = torch.empty(3 * n, dtype=torch.int32, device=cuda_device)
+    row = torch.arange(n, dtype=torch.int32, device=cuda_device).repeat(3)
+
+    def step(c, held):
+        pos.copy_(held.repeat_interleave(n, output_size=3 * n) + row)
+        c.cache.append(k, v, held, rope=rope, positions=pos)
+        c.cache.attend(rope.apply(q, pos), held + n, out=out)
+        held += n
+
+    side = torch.cuda.Stream()
+    graph, held_g = torch.cuda.CUDAGraph(), held.clone()
+    for t, x in zip((k, v, q), new):
+        t.copy_(x[0])
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        step(other, held_g)
+    for i in range(steps):
+        for t, x in zip((k, v, q), new):
+            t.copy_(x[i])
+        step(eager, held)
+        want = out.clone()
+        graph.replay()
+        assert torch.equal(out, want), i
+    assert held.tolist() == held_g.tolist() == [s + steps * n for s in start]
+    assert eager.cache.device_status() == other.cache.device_status() == 0
+    eager.held = held.tolist()
+    pages = [p for _, _, p in eager.written()]
+    for name in ("k_codes", "v_codes"):
+        a, b = (getattr(x.cache, name).view(torch.uint8)[pages] for x in (eager, other))
+        assert torch.equal(a, b), name
